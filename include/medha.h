@@ -248,6 +248,54 @@ int medha_kv_append(const void* k_new, const void* v_new, const medha_kv_cache* 
                     void* hip_stream);
 
 /*
+ * The 8-bit KV cache: half the bytes of the bf16 one.  A row -- one token's head_dim elements of
+ * one KV head -- is held as e4m3 values (OCP fp8: 1 sign, 4 exponent, 3 mantissa bits) and one
+ * scale byte: an element is value * 2^(byte - 127).  With E the exponent field of the row's
+ * largest finite magnitude,
+ *     byte  = max(E - 7, 10)
+ *     value = x * 2^(127 - byte), rounded to the nearest e4m3 value, ties to even.
+ * The largest value lies in [128, 256]: nothing saturates.  An element is off by at most 2^-4 of
+ * itself, or by 2^-10 * 2^(byte - 127) where that is more (elements below 2^-13 of the row's
+ * largest).  Infinities and NaN become NaN (of either sign); magnitudes above 1.875 * 2^127 become that.
+ */
+typedef struct medha_kv_cache_fp8 {
+  const void* k_pool; /* dev e4m3 [num_pages][num_kv_heads][page_size][head_dim], 16-byte aligned */
+  const void* v_pool; /* dev e4m3, same shape                                                    */
+  const void* scale;  /* dev uint8 [num_pages][num_kv_heads][2][page_size], keys' bytes before the
+                         values', 16-byte aligned                                                */
+  int32_t num_pages;
+  int32_t page_size;    /* must be 16 */
+  int32_t num_kv_heads;
+  int32_t head_dim;     /* 64 or 128 */
+} medha_kv_cache_fp8;
+
+/*
+ * medha_kv_append into the 8-bit cache: the same arguments (k_new and v_new are bf16) and the same
+ * handling of pages outside [0, num_pages).  Each row is quantised by itself, so a cache does not
+ * depend on how its tokens were cut into calls.  This is the one call that WRITES the cache.
+ */
+int medha_kv_append_fp8(const void* k_new, const void* v_new, const medha_kv_cache_fp8* kv,
+                        const int32_t* page_table, const int64_t* page_table_offs,
+                        const int32_t* prefix_len, const int32_t* chunk_len, int32_t batch,
+                        void* hip_stream);
+
+/*
+ * The way back: tokens first[b] .. first[b] + count[b] - 1 of every sequence, in order, as bf16
+ * rows (exactly the values the cache stands for), to hand a prefix to a bf16 cache, another GPU or
+ * host memory.
+ *
+ *   page_table, page_table_offs  as above; sequence b's slice holds at least
+ *                    ceil((first[b] + count[b]) / 16) entries
+ *   first, count     host int32 [batch], >= 0
+ *   k_out, v_out     dev bf16 [sum count][num_kv_heads][head_dim], 16-byte aligned
+ *
+ * Tokens of a page outside [0, num_pages) are zero.
+ */
+int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
+                      const int64_t* page_table_offs, const int32_t* first, const int32_t* count,
+                      int32_t batch, void* k_out, void* v_out, void* hip_stream);
+
+/*
  * Introspection of the launch plan (host only; needs no GPU).  How the library
  * would lay a chunked-prefill batch out over workgroups on a device with
  * num_cus compute units (0 = the current device, or 256 if there is none):

@@ -17,6 +17,8 @@ from .binding import (  # noqa: F401
     describe_plan_slot,
     describe_slot,
     kv_append,
+    kv_append_fp8,
+    kv_read_fp8,
     library_path,
     load_library,
     lse_merge,

@@ -33,6 +33,8 @@ EXPORTS = (
     "medha_chunk_partial_workspace_bytes",
     "medha_lse_merge",
     "medha_kv_append",
+    "medha_kv_append_fp8",
+    "medha_kv_read_fp8",
     "medha_describe_plan",
     "medha_describe_plan_slot",
     "medha_describe_slot",
@@ -57,6 +59,13 @@ class _KvCache(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
                 ("num_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _KvCacheFp8(ctypes.Structure):
+    _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
 
 
 def library_path() -> str:
@@ -97,6 +106,10 @@ def load_library():
     lib.medha_lse_merge.argtypes = [vp, vp, i32, i64, i32, i32, vp, vp, vp]
     lib.medha_kv_append.restype = ctypes.c_int
     lib.medha_kv_append.argtypes = [vp, vp, ctypes.POINTER(_KvCache), vp, vp, vp, vp, i32, vp]
+    lib.medha_kv_append_fp8.restype = ctypes.c_int
+    lib.medha_kv_append_fp8.argtypes = [vp, vp, ctypes.POINTER(_KvCacheFp8), vp, vp, vp, vp, i32, vp]
+    lib.medha_kv_read_fp8.restype = ctypes.c_int
+    lib.medha_kv_read_fp8.argtypes = [ctypes.POINTER(_KvCacheFp8), vp, vp, vp, vp, i32, vp, vp, vp]
     lib.medha_describe_plan.restype = ctypes.c_int
     lib.medha_describe_plan.argtypes = [vp, vp, i32, i32, i32, i32, i32, ctypes.POINTER(PlanEntry),
                                         ctypes.POINTER(i32), ctypes.POINTER(i32),
@@ -125,6 +138,7 @@ class _LongWay:
         return None
 
     chunked_prefill_attn = decode_partial_attn = chunk_partial_attn = lse_merge = kv_append = _none
+    kv_append_fp8 = kv_read_fp8 = _none
 
 
 def _extension_module(lib):
@@ -141,12 +155,14 @@ def _extension_module(lib):
                       "(build it with `python -m paper_2409_17264_amd.build`)", RuntimeWarning,
                       stacklevel=3)
         return _LongWay
-    calls = ("medha_chunked_prefill_attn", "medha_chunked_prefill_attn_alloc",
-             "medha_decode_partial_attn", "medha_decode_partial_workspace_bytes",
-             "medha_chunk_partial_attn", "medha_chunk_partial_workspace_bytes", "medha_lse_merge",
-             "medha_kv_append")
-    _marshal.bind(_stream, _check,
-                  *(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in calls))
+    def addresses(*names):
+        return (ctypes.cast(getattr(lib, "medha_" + name), ctypes.c_void_p).value for name in names)
+
+    _marshal.bind(_stream, _check, *addresses(
+        "chunked_prefill_attn", "chunked_prefill_attn_alloc", "decode_partial_attn",
+        "decode_partial_workspace_bytes", "chunk_partial_attn", "chunk_partial_workspace_bytes",
+        "lse_merge", "kv_append"))
+    _marshal.bind_fp8(torch.cuda.current_device, *addresses("kv_append_fp8", "kv_read_fp8"))
     return _marshal
 
 
@@ -197,6 +213,31 @@ def _kv(k_pool: torch.Tensor, v_pool: torch.Tensor) -> _KvCache:
     assert k_pool.is_contiguous() and v_pool.is_contiguous() and k_pool.shape == v_pool.shape
     num_pages, h_kv, page_size, d = k_pool.shape
     return _KvCache(k_pool.data_ptr(), v_pool.data_ptr(), num_pages, page_size, h_kv, d)
+
+
+def _same_device(*tensors: torch.Tensor) -> None:
+    """All on the current device, whose stream the call is enqueued on."""
+    here = torch.cuda.current_device()
+    assert all(t.is_cuda and t.get_device() == here for t in tensors)
+
+
+def _kv_fp8(k_pool: torch.Tensor, v_pool: torch.Tensor, kv_scale: torch.Tensor) -> _KvCacheFp8:
+    assert k_pool.dtype == torch.float8_e4m3fn and v_pool.dtype == torch.float8_e4m3fn
+    assert kv_scale.dtype == torch.uint8 and k_pool.shape == v_pool.shape
+    assert k_pool.is_contiguous() and v_pool.is_contiguous() and kv_scale.is_contiguous()
+    num_pages, h_kv, page_size, d = k_pool.shape
+    assert kv_scale.shape == (num_pages, h_kv, 2, page_size)
+    _same_device(k_pool, v_pool, kv_scale)
+    return _KvCacheFp8(k_pool.data_ptr(), v_pool.data_ptr(), kv_scale.data_ptr(), num_pages,
+                       page_size, h_kv, d)
+
+
+def _pages(page_table: torch.Tensor, page_table_offs, batch: int) -> np.ndarray:
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous()
+    _same_device(page_table)
+    offs = _host(page_table_offs, np.int64)
+    assert len(offs) == batch + 1 and int(offs[-1]) <= page_table.numel()
+    return offs
 
 
 def chunked_prefill_workspace_bytes(prefix_len, chunk_len, num_q_heads: int, num_kv_heads: int,
@@ -460,3 +501,54 @@ def kv_append(k_new: torch.Tensor, v_new: torch.Tensor, k_pool: torch.Tensor,
     assert int(offs[-1]) <= page_table.numel()
     _check(lib.medha_kv_append(_dp(k_new), _dp(v_new), ctypes.byref(kv), _dp(page_table),
                                _hp(offs), _hp(pre), _hp(chk), batch, _stream()))
+
+
+def kv_append_fp8(k_new: torch.Tensor, v_new: torch.Tensor, k_pool: torch.Tensor,
+                  v_pool: torch.Tensor, kv_scale: torch.Tensor, page_table: torch.Tensor,
+                  page_table_offs, prefix_len, chunk_len) -> None:
+    """k_new, v_new bf16 [tokens][h_kv][d] (device) are quantised into the 8-bit cache in place:
+    pools float8_e4m3fn [pages][h_kv][16][d], kv_scale uint8 [pages][h_kv][2][16] (a row's
+    exponent byte, K's before V's: an element is value * 2^(byte - 127))."""
+    lib = load_library()
+    done = _NATIVE.kv_append_fp8(k_new, v_new, k_pool, v_pool, kv_scale, page_table,
+                                 page_table_offs, prefix_len, chunk_len)
+    if done is not None:
+        return None
+    for t in (k_new, v_new):
+        assert t.dtype == torch.bfloat16 and t.is_contiguous() and t.dim() == 3
+    assert k_new.shape == v_new.shape
+    _same_device(k_new, v_new)
+    kv = _kv_fp8(k_pool, v_pool, kv_scale)
+    tokens, h_kv, d = k_new.shape
+    assert h_kv == kv.num_kv_heads and d == kv.head_dim
+    pre, chk = _host(prefix_len, np.int32), _host(chunk_len, np.int32)
+    offs = _pages(page_table, page_table_offs, len(pre))
+    assert len(chk) == len(pre) and _total(chk) == tokens
+    _check(lib.medha_kv_append_fp8(_dp(k_new), _dp(v_new), ctypes.byref(kv), _dp(page_table),
+                                   _hp(offs), _hp(pre), _hp(chk), len(pre), _stream()))
+
+
+def kv_read_fp8(k_pool: torch.Tensor, v_pool: torch.Tensor, kv_scale: torch.Tensor,
+                page_table: torch.Tensor, page_table_offs, first, count,
+                k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+    """Tokens first .. first + count - 1 of every sequence out of the 8-bit cache.  Returns
+    (k, v), bf16 [sum count][h_kv][d]: what the cache holds, exactly."""
+    lib = load_library()
+    done = _NATIVE.kv_read_fp8(k_pool, v_pool, kv_scale, page_table, page_table_offs, first, count,
+                               k_out, v_out)
+    if done is not None:
+        return done
+    kv = _kv_fp8(k_pool, v_pool, kv_scale)
+    fst, cnt = _host(first, np.int32), _host(count, np.int32)
+    offs = _pages(page_table, page_table_offs, len(fst))
+    assert len(cnt) == len(fst) and (len(cnt) == 0 or cnt.min() >= 0)
+    shape = (_total(cnt), kv.num_kv_heads, kv.head_dim)
+    k_out, v_out = (torch.empty(shape, dtype=torch.bfloat16, device=k_pool.device) if t is None
+                    else t for t in (k_out, v_out))
+    for t in (k_out, v_out):
+        assert t.dtype == torch.bfloat16 and t.is_contiguous() and t.shape == shape
+    _same_device(k_out, v_out)
+    if shape[0] > 0:
+        _check(lib.medha_kv_read_fp8(ctypes.byref(kv), _dp(page_table), _hp(offs), _hp(fst),
+                                     _hp(cnt), len(fst), _dp(k_out), _dp(v_out), _stream()))
+    return k_out, v_out

@@ -1,6 +1,6 @@
-"""Compile the HIP libraries for gfx950: csrc/medha.hip into libmedha.so (the product)
-and csrc/yardstick.hip into libmedha_yardstick.so (the benchmark's yardsticks), and the
-binding's host code, csrc/marshal.cpp, into the extension module _marshal.
+"""Compile the HIP libraries for gfx950: csrc/medha.hip and csrc/window_fp8.hip into libmedha.so
+(the product) and csrc/yardstick.hip into libmedha_yardstick.so (the benchmark's yardsticks), and
+the binding's host code, csrc/marshal.cpp, into the extension module _marshal.
 
 The libraries need hipcc alone.  The module needs g++, the headers of this interpreter (Python 3.10
 or later) and of torch, and works with the interpreter and the torch that it is built with: its
@@ -14,18 +14,21 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libmedha.so")
-# source file -> shared library
-TARGETS = {"medha.hip": LIB, "yardstick.hip": os.path.join(HERE, "libmedha_yardstick.so")}
+# shared library -> source files
+TARGETS = {LIB: ("medha.hip", "window_fp8.hip"),
+           os.path.join(HERE, "libmedha_yardstick.so"): ("yardstick.hip",)}
 
 MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 HIPCC_FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function", "-Wno-inline-asm", "-fno-gpu-rdc",
 ]
@@ -60,10 +63,16 @@ def _marshal_command():
 def build(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     found = sorted(os.path.basename(p) for p in glob.glob(os.path.join(CSRC, "*.hip")))
-    assert found == sorted(TARGETS), f"every .hip source needs a target: {found}"
-    for src, lib in TARGETS.items():
-        _run([hipcc] + HIPCC_FLAGS + ["-I", INCLUDE, "-I", CSRC, os.path.join(CSRC, src), "-o", lib],
-             src, verbose)
+    sources = sorted(s for srcs in TARGETS.values() for s in srcs)
+    assert found == sources, f"every .hip source needs a target: {found}"
+    flags = HIPCC_FLAGS + ["-I", INCLUDE, "-I", CSRC]
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor() as pool:
+        objects = {src: os.path.join(tmp, src + ".o") for src in sources}
+        list(pool.map(lambda src: _run([hipcc] + flags + ["-c", os.path.join(CSRC, src), "-o",
+                                                          objects[src]], src, verbose), sources))
+        for lib, srcs in TARGETS.items():
+            _run([hipcc] + flags + ["-shared", *(objects[s] for s in srcs), "-o", lib],
+                 os.path.basename(lib), verbose)
     _run(_marshal_command(), "marshal.cpp", verbose)
     return LIB
 

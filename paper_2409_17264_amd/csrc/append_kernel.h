@@ -8,15 +8,6 @@
 
 namespace medha {
 
-struct AppendDesc {
-  int64_t pt_off;      // first entry of the sequence in the page table
-  int32_t src_row;     // first token row of the sequence in k_new / v_new
-  int32_t prefix_len;  // tokens already in the cache: token j goes to position prefix_len + j
-  int32_t chunk_len;
-  int32_t row_rank;    // rank of the sequence's first token row among the launch's rows
-};
-static_assert(sizeof(AppendDesc) == 24, "AppendDesc layout");
-
 struct AppendArgs {
   const uint4* k_new;
   const uint4* v_new;

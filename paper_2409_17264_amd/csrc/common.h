@@ -13,6 +13,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -86,6 +87,16 @@ struct MergeArgs {
   SeqDesc inline_descs[kMaxInlineSeq];
 };
 static_assert(sizeof(MergeArgs) <= 4096, "kernel argument block too large");
+
+// One sequence of a launch that moves tokens between dense rows and the paged pools.
+struct AppendDesc {
+  int64_t pt_off;      // first entry of the sequence in the page table
+  int32_t src_row;     // first token row of the sequence in k_new / v_new
+  int32_t prefix_len;  // tokens already in the cache: token j goes to position prefix_len + j
+  int32_t chunk_len;
+  int32_t row_rank;    // rank of the sequence's first token row among the launch's rows
+};
+static_assert(sizeof(AppendDesc) == 24, "AppendDesc layout");
 
 // Workgroup slot u of a sequence -> its work item.  Slot u runs on die u % 8
 // (the hardware deals consecutive workgroups round-robin to the 8 dies).  The

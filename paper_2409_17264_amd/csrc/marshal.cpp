@@ -37,7 +37,10 @@ struct Library {
   decltype(&medha_chunk_partial_workspace_bytes) chunk_bytes = nullptr;
   decltype(&medha_lse_merge) merge = nullptr;
   decltype(&medha_kv_append) append = nullptr;
+  decltype(&medha_kv_append_fp8) append_fp8 = nullptr;
+  decltype(&medha_kv_read_fp8) read_fp8 = nullptr;
   PyObject* stream = nullptr;
+  PyObject* device = nullptr;  // index of the current one
   PyObject* check = nullptr;  // raises an error code of the library's
 } lib;
 
@@ -150,6 +153,24 @@ bool cache(PyObject* k, PyObject* v, medha_kv_cache& kv) {
   return true;
 }
 
+// The calls on the 8-bit cache and on windows take tensors of one device, the current one's stream
+// being asked for that device.
+bool on_device(const at::Tensor* t, c10::DeviceIndex index) { return t->get_device() == index; }
+
+bool cache_fp8(PyObject* k, PyObject* v, PyObject* s, medha_kv_cache_fp8& kv) {
+  const at::Tensor *kt = tensor(k), *vt = tensor(v), *st = tensor(s);
+  if (!device_array(kt, at::kFloat8_e4m3fn, 4) || !device_array(vt, at::kFloat8_e4m3fn, 4) ||
+      !device_array(st, at::kByte, 4) || kt->sizes() != vt->sizes() || st->size(0) != kt->size(0) ||
+      st->size(1) != kt->size(1) || st->size(2) != 2 || st->size(3) != kt->size(2) ||
+      !on_device(vt, kt->get_device()) || !on_device(st, kt->get_device()))
+    return false;
+  for (int i = 0; i < 4; ++i)
+    if (kt->size(i) > std::numeric_limits<int32_t>::max()) return false;
+  kv = medha_kv_cache_fp8{kt->data_ptr(), vt->data_ptr(), st->data_ptr(), (int32_t)kt->size(0),
+                          (int32_t)kt->size(2), (int32_t)kt->size(1), (int32_t)kt->size(3)};
+  return true;
+}
+
 // Page table and offsets of n sequences.
 bool pages(const at::Tensor* table, const HostArray<int64_t>& offs, int64_t n) {
   return device_array(table, at::kInt, -1) && n >= 1 && n < std::numeric_limits<int32_t>::max() &&
@@ -166,13 +187,14 @@ bool room(PyObject* o, at::Tensor& t) {
 }
 
 // An output: the caller's tensor, checked, or a new one.
-bool output(PyObject* o, at::IntArrayRef sizes, const at::Tensor& like, at::Tensor& t) {
+bool output(PyObject* o, at::IntArrayRef sizes, const at::Tensor& like, at::Tensor& t,
+            at::ScalarType type = at::kFloat) {
   if (o == Py_None) {
-    t = at::empty(sizes, like.options().dtype(at::kFloat));
+    t = at::empty(sizes, like.options().dtype(type));
     return true;
   }
   const at::Tensor* given = tensor(o);
-  if (!device_array(given, at::kFloat, -1) || given->sizes() != sizes) return false;
+  if (!device_array(given, type, -1) || given->sizes() != sizes) return false;
   t = *given;
   return true;
 }
@@ -202,6 +224,16 @@ bool current_stream(void*& stream) {
   stream = PyLong_AsVoidPtr(s);
   Py_DECREF(s);
   return !PyErr_Occurred();
+}
+
+// The current stream, if `index` is the current device.
+bool current_stream_of(c10::DeviceIndex index, void*& stream) {
+  if (lib.device == nullptr) return false;
+  PyObject* d = PyObject_CallNoArgs(lib.device);
+  if (d == nullptr) return false;
+  const long current = PyLong_AsLong(d);
+  Py_DECREF(d);
+  return !PyErr_Occurred() && current == index && current_stream(stream);
 }
 
 // Runs `call` as the binding's steps are run: a C++ error (a tensor without storage, memory that is
@@ -433,6 +465,77 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// (k_new, v_new, k_pool, v_pool, kv_scale, page_table, offs, prefix_len, chunk_len); True when done
+PyObject* kv_append_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return ordinary([&]() -> PyObject* {
+    const at::Tensor *k, *v, *table;
+    medha_kv_cache_fp8 kv;
+    HostArray<int64_t> offs;
+    HostArray<int32_t> pre, chk;
+    void* stream;
+    if (n != 9 || !pre.take(a[7]) || !chk.take(a[8]) || !offs.take(a[6]) ||
+        !device_array(k = tensor(a[0]), at::kBFloat16, 3) ||
+        !device_array(v = tensor(a[1]), at::kBFloat16, 3) || k->sizes() != v->sizes() ||
+        !cache_fp8(a[2], a[3], a[4], kv) || k->size(1) != kv.num_kv_heads ||
+        k->size(2) != kv.head_dim || chk.size() != pre.size() ||
+        !pages(table = tensor(a[5]), offs, pre.size()) || total(chk) != k->size(0) ||
+        !on_device(v, k->get_device()) || !on_device(table, k->get_device()) ||
+        !on_device(tensor(a[2]), k->get_device()) || !current_stream_of(k->get_device(), stream))
+      return nullptr;
+    const void *kp = k->data_ptr(), *vp = v->data_ptr();
+    const int32_t* tp = static_cast<const int32_t*>(table->data_ptr());
+    int rc;
+    {
+      Unlocked unlocked;
+      rc = lib.append_fp8(kp, vp, &kv, tp, offs.data(), pre.data(), chk.data(), (int32_t)pre.size(),
+                          stream);
+    }
+    return made(rc) ? Py_NewRef(Py_True) : nullptr;
+  });
+}
+
+// (k_pool, v_pool, kv_scale, page_table, offs, first, count, k_out, v_out)
+PyObject* kv_read_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return ordinary([&]() -> PyObject* {
+    const at::Tensor* table;
+    medha_kv_cache_fp8 kv;
+    HostArray<int64_t> offs;
+    HostArray<int32_t> first, count;
+    void* stream;
+    if (n != 9 || !first.take(a[5]) || !count.take(a[6]) || !offs.take(a[4]) ||
+        !cache_fp8(a[0], a[1], a[2], kv) || count.size() != first.size() ||
+        !pages(table = tensor(a[3]), offs, first.size()))
+      return nullptr;
+    const at::Tensor& pool = *tensor(a[0]);
+    const int64_t sizes[3] = {total(count), kv.num_kv_heads, kv.head_dim};
+    if (sizes[0] <= 0) return nullptr;
+    for (int64_t i = 0; i < count.size(); ++i)
+      if (count.data()[i] < 0) return nullptr;
+    at::Tensor k, v;
+    if (!output(a[7], at::IntArrayRef(sizes, 3), pool, k, at::kBFloat16) ||
+        !output(a[8], at::IntArrayRef(sizes, 3), pool, v, at::kBFloat16) ||
+        !on_device(&k, pool.get_device()) || !on_device(&v, pool.get_device()) ||
+        !on_device(table, pool.get_device()) || !current_stream_of(pool.get_device(), stream))
+      return nullptr;
+    void *kp = k.data_ptr(), *vp = v.data_ptr();
+    const int32_t* tp = static_cast<const int32_t*>(table->data_ptr());
+    int rc;
+    {
+      Unlocked unlocked;
+      rc = lib.read_fp8(&kv, tp, offs.data(), first.data(), count.data(), (int32_t)first.size(), kp,
+                        vp, stream);
+    }
+    return made(rc) ? pair(a[7], k, a[8], v) : nullptr;
+  });
+}
+
+// Reads entry points' addresses; false with a Python error.
+template <int kEntries>
+bool addresses(PyObject* const* a, void* (&p)[kEntries]) {
+  for (int i = 0; i < kEntries; ++i) p[i] = PyLong_AsVoidPtr(a[i]);
+  return !PyErr_Occurred();
+}
+
 // bind(stream, check, entry points' addresses in the order below)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   constexpr int kEntries = 8;
@@ -441,8 +544,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   }
   void* p[kEntries];
-  for (int i = 0; i < kEntries; ++i) p[i] = PyLong_AsVoidPtr(a[i + 2]);
-  if (PyErr_Occurred()) return nullptr;
+  if (!addresses(a + 2, p)) return nullptr;
   lib.prefill = reinterpret_cast<decltype(lib.prefill)>(p[0]);
   lib.prefill_alloc = reinterpret_cast<decltype(lib.prefill_alloc)>(p[1]);
   lib.decode = reinterpret_cast<decltype(lib.decode)>(p[2]);
@@ -456,9 +558,25 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// bind_fp8(function for the current device's index, entry points' addresses in the order below)
+PyObject* bind_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  constexpr int kEntries = 2;
+  if (n != 1 + kEntries) {
+    PyErr_Format(PyExc_TypeError, "bind_fp8() takes %d arguments", 1 + kEntries);
+    return nullptr;
+  }
+  void* p[kEntries];
+  if (!addresses(a + 1, p)) return nullptr;
+  lib.append_fp8 = reinterpret_cast<decltype(lib.append_fp8)>(p[0]);
+  lib.read_fp8 = reinterpret_cast<decltype(lib.read_fp8)>(p[1]);
+  Py_XSETREF(lib.device, Py_NewRef(a[0]));
+  Py_RETURN_NONE;
+}
+
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CALL(bind), CALL(chunked_prefill_attn), CALL(decode_partial_attn),
+PyMethodDef methods[] = {CALL(bind), CALL(bind_fp8), CALL(chunked_prefill_attn), CALL(decode_partial_attn),
                          CALL(chunk_partial_attn), CALL(lse_merge), CALL(kv_append),
+                         CALL(kv_append_fp8), CALL(kv_read_fp8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 

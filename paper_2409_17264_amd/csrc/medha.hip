@@ -13,6 +13,7 @@
 #include "append_kernel.h"
 #include "common.h"
 #include "decode_kernel.h"
+#include "host.h"
 #include "merge_kernel.h"
 #include "planner.h"
 #include "policy.h"
@@ -49,25 +50,6 @@ void* noalloc_scratch_ptr(int* rc) {
   }
   *rc = MEDHA_OK;
   return ptr[dev];
-}
-
-int current_num_cus() {
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess ||
-      cus <= 0) {
-    (void)hipGetLastError();
-    return 256;  // MI355X; used only for planning queries made without a device
-  }
-  return cus;
-}
-
-bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-int check_heads(int h_q, int h_kv, int d, int page_size) {
-  if (h_q <= 0 || h_kv <= 0 || h_q % h_kv != 0) return MEDHA_ERR_INVALID_ARG;
-  if (page_size != kPageSize || (d != 64 && d != 128)) return MEDHA_ERR_UNSUPPORTED;
-  return MEDHA_OK;
 }
 
 template <int D, int STAGES>
@@ -207,11 +189,6 @@ int check_kv(const medha_kv_cache* kv, int h_q) {
     return MEDHA_ERR_INVALID_ARG;
   if (!aligned(kv->k_pool, 16) || !aligned(kv->v_pool, 16)) return MEDHA_ERR_INVALID_ARG;
   return check_heads(h_q, kv->num_kv_heads, kv->head_dim, kv->page_size);
-}
-
-// The part of a caller's workspace a plan may count on: none of a missing or misaligned one.
-size_t usable_bytes(const void* workspace, size_t bytes) {
-  return workspace != nullptr && aligned(workspace, 256) ? bytes : 0;
 }
 
 // Scratch of a chunked-prefill call: what its fastest plan takes, or the least it can do with

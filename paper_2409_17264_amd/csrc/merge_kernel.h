@@ -78,7 +78,7 @@ __device__ __forceinline__ void merge_one(const float* __restrict__ part_o,
 }
 
 // Public merge: uniform split count, partials [n_split][rows][h_q][d].
-__global__ void __launch_bounds__(kThreads) lse_merge_kernel(
+static __global__ void __launch_bounds__(kThreads) lse_merge_kernel(
     const float* __restrict__ part_o, const float* __restrict__ part_lse, int n_split,
     int64_t rows, int h_q, int d, float* __restrict__ out, float* __restrict__ lse) {
   const int per_row = d / 4;

@@ -1,0 +1,234 @@
+"""The 8-bit KV cache: quantising append and read back, bit for bit against the oracle."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.fp8 as ref
+import paper_2409_17264_amd as medha
+from paper_2409_17264_amd import workloads as wl
+
+FP8 = torch.float8_e4m3fn
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def all_rows(d):
+    """bf16 rows whose elements run through every bit pattern, the finite ones sorted by magnitude so
+    that a row's elements have one another's exponents, and shuffled ones that mix them."""
+    every = np.arange(1 << 16, dtype=np.uint16)
+    near = every[np.argsort(every & 0x7fff, kind="stable")]
+    far = np.random.default_rng(3).permutation(every)
+    return np.concatenate([near, far]).reshape(-1, d)
+
+
+# ----------------------------------------------------------------- the oracle itself (CPU)
+
+def test_oracle_codes_are_the_e4m3_of_torch():
+    codes = torch.arange(256, dtype=torch.uint8)
+    assert np.array_equal(ref.e4m3_values(codes.numpy()), codes.view(FP8).double().numpy(),
+                          equal_nan=True)
+    x = torch.cat([torch.linspace(-448, 448, 100001), torch.randn(50000) * 0.01,
+                   torch.tensor([0.0, -0.0, 2.0 ** -10, -(2.0 ** -10), 3 * 2.0 ** -10])])
+    assert np.array_equal(ref.e4m3_codes(x.double().numpy()), x.to(FP8).view(torch.uint8).numpy())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_oracle_rows_keep_to_the_documented_error(d):
+    rows = all_rows(d)
+    code, byte = ref.quantise_rows(rows)
+    x, y = ref.bf16_values(rows), np.ldexp(ref.e4m3_values(code), byte.astype(int)[..., None] - 127)
+    fine = np.isfinite(x)
+    assert np.array_equal(fine, np.isfinite(y)) and np.isnan(y[~fine]).all()
+    x = np.clip(np.where(fine, x, 0.0), -1.875 * 2.0 ** 127, 1.875 * 2.0 ** 127)
+    y = np.where(fine, y, 0.0)
+    bound = np.maximum(np.abs(x) * 2.0 ** -4, np.ldexp(1.0, byte.astype(int) - 137)[..., None])
+    assert (np.abs(y - x) <= bound).all()
+    top = np.abs(ref.e4m3_values(code))
+    top = np.where(np.isnan(top), 0, top).max(-1)
+    assert (top <= 256).all() and (top[byte > 10] >= 120).all() and (byte >= 10).all()
+    as_bf16 = torch.from_numpy(y).to(torch.bfloat16).double().numpy()
+    assert np.array_equal(as_bf16, y)  # reading back loses nothing
+
+
+# ----------------------------------------------------------------- refusals (CPU: nothing is enqueued)
+
+def _host_call(name, **change):
+    """The C entry with addresses that no kernel ever gets to see."""
+    import ctypes
+    from paper_2409_17264_amd import binding
+    lib = medha.load_library()
+    at = 1 << 20
+    a = dict(rows_k=at, rows_v=at, k=at, v=at, s=at, pages=8, size=16, heads=2, d=64, table=at,
+             offs=[0, 4], first=[3], count=[20], batch=1)
+    a.update(change)
+    kv = binding._KvCacheFp8(a["k"], a["v"], a["s"], a["pages"], a["size"], a["heads"], a["d"])
+    host = [np.array(a[n], t).tobytes() if a[n] is not None else None
+            for n, t in (("offs", np.int64), ("first", np.int32), ("count", np.int32))]
+    kvp = ctypes.byref(kv) if not change.get("null") else None
+    if name == "append":
+        return lib.medha_kv_append_fp8(a["rows_k"], a["rows_v"], kvp, a["table"], *host, a["batch"], None)
+    return lib.medha_kv_read_fp8(kvp, a["table"], *host, a["batch"], a["rows_k"], a["rows_v"], None)
+
+
+@pytest.mark.parametrize("name", ["append", "read"])
+@pytest.mark.parametrize("change, code", [
+    (dict(null=True), -1), (dict(rows_k=None), -1), (dict(rows_v=None), -1), (dict(k=None), -1),
+    (dict(v=None), -1), (dict(s=None), -1), (dict(table=None), -1), (dict(offs=None), -1),
+    (dict(first=None), -1), (dict(count=None), -1), (dict(batch=-1), -1), (dict(heads=0), -1),
+    (dict(pages=-1), -1), (dict(rows_k=(1 << 20) + 8), -1), (dict(k=(1 << 20) + 8), -1),
+    (dict(s=(1 << 20) + 8), -1), (dict(size=32), -2), (dict(d=96), -2), (dict(first=[-1]), -1),
+    (dict(count=[-1]), -1), (dict(first=[2 ** 31 - 10]), -1), (dict(offs=[0, 1]), -1),
+    (dict(offs=[-1, 4]), -1), (dict(offs=[3, 4]), -1), (dict(batch=0), 0)])
+def test_refusals(name, change, code):
+    assert _host_call(name, **change) == code
+
+
+def test_empty_reads_and_appends():
+    assert _host_call("append", count=[0]) == -1   # as the bf16 append
+    assert _host_call("read", count=[0]) == 0      # nothing to do, nothing launched
+
+
+def test_tensors_off_the_device_are_refused():
+    k = torch.zeros(4, 2, 16, 64, dtype=torch.uint8).view(FP8)
+    s = torch.zeros(4, 2, 2, 16, dtype=torch.uint8)
+    new = torch.zeros(5, 2, 64, dtype=torch.bfloat16)
+    table = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises((AssertionError, RuntimeError)):
+        medha.kv_append_fp8(new, new, k, k.clone(), s, table, [0, 1], [0], [5])
+    with pytest.raises((AssertionError, RuntimeError)):
+        medha.kv_read_fp8(k, k.clone(), s, table, [0, 1], [0], [5])
+
+
+# ----------------------------------------------------------------- on the device
+
+def _cache(pages, h_kv, d, fill=0xA5):
+    pool = torch.full((2, pages, h_kv, 16, d), fill, dtype=torch.uint8, device="cuda")
+    return pool[0].view(FP8), pool[1].view(FP8), torch.full((pages, h_kv, 2, 16), fill,
+                                                            dtype=torch.uint8, device="cuda")
+
+
+def _codes(k, v, s):
+    return [t.view(torch.uint8).cpu().numpy().copy() for t in (k, v, s)]
+
+
+def _append_both(k_new, v_new, prefix, chunk, d, seed=1, pages=None, table=None):
+    h_kv = k_new.shape[1]
+    need = [wl.pages_for(p + c) for p, c in zip(prefix, chunk)]
+    pages = pages or sum(need) + 3
+    if table is None:
+        table, _ = wl.permuted_page_tables([sum(need)], pages, seed)
+    offs = np.concatenate([[0], np.cumsum(need)]).astype(np.int64)
+    cache = _cache(pages, h_kv, d)
+    want = _codes(*cache)
+    medha.kv_append_fp8(torch.from_numpy(k_new.view(np.int16)).view(torch.bfloat16).cuda(),
+                        torch.from_numpy(v_new.view(np.int16)).view(torch.bfloat16).cuda(), *cache,
+                        torch.from_numpy(table).cuda(), offs, prefix, chunk)
+    torch.cuda.synchronize()
+    ref.kv_append_fp8(k_new, v_new, *want, table, offs, prefix, chunk)
+    return cache, want, table, offs
+
+
+def _equal_codes(got, want):
+    """Equal bit for bit, a NaN's sign apart (0x7f and 0xff: e4m3 has no other)."""
+    for g, w in zip(got[:2], want[:2]):
+        nan = (w & 127) == 127
+        assert np.array_equal((g & 127) == 127, nan)
+        assert np.array_equal(g[~nan], w[~nan])
+    assert np.array_equal(got[2], want[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_quantises_every_bf16_value_as_defined(d):
+    rows = all_rows(d)
+    k, v = rows.reshape(-1, 2, d), rows[::-1].reshape(-1, 2, d).copy()
+    cache, want, table, offs = _append_both(k, v, [5], [len(k)], d)
+    _equal_codes(_codes(*cache), want)
+    # and back: the values the codes stand for, in bf16, exactly
+    got = medha.kv_read_fp8(*cache, torch.from_numpy(table).cuda(), offs, [5], [len(k)])
+    for g, w in zip(got, ref.kv_read_fp8(*want, table, offs, [5], [len(k)])):
+        assert np.array_equal(g.double().cpu().numpy(), w, equal_nan=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("h_kv, d", [(1, 64), (3, 128), (8, 128), (2, 64)])
+@pytest.mark.parametrize("prefix, chunk", [
+    ([0], [1]), ([15], [1]), ([16], [1]), ([7], [40]), ([0, 31, 100, 5], [16, 17, 1, 300]),
+    (list(range(70)), [1] * 70), (list(range(0, 130, 2)), [3] * 65)])
+def test_append_and_read_of_ragged_batches(h_kv, d, prefix, chunk):
+    rng = np.random.default_rng(len(prefix) + d)
+    n = sum(chunk)
+    k, v = (ref_bits(rng.standard_normal((n, h_kv, d)) * np.exp(rng.standard_normal((n, h_kv, 1)) * 4))
+            for _ in range(2))
+    cache, want, table, offs = _append_both(k, v, prefix, chunk, d)
+    _equal_codes(_codes(*cache), want)  # slots of no token, and pages of no table, are as they were
+    first = [max(0, p - 3) for p in prefix]
+    count = [p + c - f if i % 3 else 0 for i, (p, c, f) in enumerate(zip(prefix, chunk, first))]
+    out = [torch.full((sum(count), h_kv, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    got = medha.kv_read_fp8(*cache, torch.from_numpy(table).cuda(), offs, first, count, *out)
+    assert got[0] is out[0] and got[1] is out[1]
+    for g, w in zip(got, ref.kv_read_fp8(*want, table, offs, first, count)):
+        assert np.array_equal(g.double().cpu().numpy(), w)
+
+
+def ref_bits(x):
+    return bits(torch.from_numpy(x).to(torch.bfloat16))
+
+
+@pytest.mark.gpu
+def test_pages_outside_the_pool_are_skipped_and_read_as_zero():
+    d, h_kv = 128, 2
+    rng = np.random.default_rng(8)
+    k, v = (ref_bits(rng.standard_normal((64, h_kv, d))) for _ in range(2))
+    table = np.array([2, -1, 9, 0], np.int32)
+    cache, want, table, offs = _append_both(k, v, [0], [64], d, pages=4, table=table)
+    _equal_codes(_codes(*cache), want)
+    got = medha.kv_read_fp8(*cache, torch.from_numpy(table).cuda(), offs, [0], [64])
+    for g, w in zip(got, ref.kv_read_fp8(*want, table, offs, [0], [64])):
+        assert np.array_equal(g.double().cpu().numpy(), w)
+        assert (g[16:48] == 0).all()
+
+
+@pytest.mark.gpu
+def test_a_cache_does_not_depend_on_how_its_tokens_were_cut():
+    d, h_kv, n = 64, 2, 333
+    rng = np.random.default_rng(9)
+    k, v = (torch.from_numpy(rng.standard_normal((n, h_kv, d))).to(torch.bfloat16).cuda() for _ in range(2))
+    table = torch.randperm(21, dtype=torch.int32).cuda()
+    whole, parts = _cache(21, h_kv, d), _cache(21, h_kv, d)
+    medha.kv_append_fp8(k, v, *whole, table, [0, 21], [0], [n])
+    at = 0
+    for c in (1, 15, 17, 100, 200):
+        medha.kv_append_fp8(k[at:at + c], v[at:at + c], *parts, table, [0, 21], [at], [c])
+        at += c
+    assert at == n
+    for a, b in zip(_codes(*whole), _codes(*parts)):
+        assert np.array_equal(a, b)
+
+
+@pytest.mark.gpu
+def test_python_refusals_on_the_device():
+    d, h_kv = 64, 2
+    cache = _cache(4, h_kv, d)
+    new = torch.zeros(5, h_kv, d, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(4, dtype=torch.int32, device="cuda")
+    ok = (new, new, *cache, table, [0, 1], [0], [5])
+    bad = [{0: new.float()}, {1: new[:4]}, {0: new[:, :1], 1: new[:, :1]}, {2: cache[0].view(torch.uint8)},
+           {4: cache[2][:3]}, {4: cache[2].view(torch.int8)}, {5: table.long()}, {6: [0, 9]}, {6: [0]},
+           {8: [4]}, {0: new.cpu(), 1: new.cpu()}, {5: table.cpu()}, {4: cache[2].cpu()}]
+    medha.kv_append_fp8(*ok)
+    for change in bad:
+        args = [change.get(i, a) for i, a in enumerate(ok)]
+        with pytest.raises(AssertionError):
+            medha.kv_append_fp8(*args)
+    ok = (*cache, table, [0, 1], [0], [5])
+    medha.kv_read_fp8(*ok)
+    for change in [{0: cache[0].view(torch.uint8)}, {2: cache[2][:3]}, {3: table.cpu()}, {4: [0, 9]},
+                   {5: [0, 0]}, {6: [-1]}, {7: new.float()}, {7: new[:4]}, {8: new.cpu()}]:
+        args = [change.get(i, a) for i, a in enumerate(ok + (None, None))]
+        with pytest.raises(AssertionError):
+            medha.kv_read_fp8(*args)
+    with pytest.raises(medha.MedhaError):
+        medha.kv_read_fp8(*cache, table, [0, 1], [0], [17])  # a page more than the slice holds
