@@ -296,6 +296,59 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
                       int32_t batch, void* k_out, void* v_out, void* hip_stream);
 
 /*
+ * medha_chunked_prefill_attn over the 8-bit cache, optionally behind a window: the row at position
+ * p of a sequence attends to keys t <= p with  t > p - window  or  t < sinks  (window 0: to all
+ * t <= p; sinks is not looked at).  The other arguments, the batches and the layouts are those of
+ * medha_chunked_prefill_attn.  O and LSE of a shard that lies before the query are those of the
+ * sequence (prefix_len = kv_len - 1, chunk_len 1) and merge with medha_lse_merge as others do.
+ *
+ *   window           keys a row sees up to and with its own, >= 1, or 0
+ *   sinks            first tokens of the sequence that every row sees, >= 0
+ *   out_type         MEDHA_OUT_FP32 or MEDHA_OUT_BF16 (rounded once, to nearest even)
+ *   out              dev  fp32 or bf16 [sum chunk_len][num_q_heads][head_dim], 16-byte aligned
+ *   workspace        as for medha_chunked_prefill_attn, of the size that
+ *                    medha_chunked_prefill_fp8_workspace_bytes reports for these arguments
+ *
+ * Arithmetic: the cache's values times q, exact products, accumulated by the matrix cores' 8-bit
+ * instructions (a score is off by some 1e-5 of the root mean square of its kind), fp32 softmax
+ * statistics, and P * V as in the bf16 calls.
+ * Only tokens that some row of the call sees are read, and only their pages' table entries are
+ * used: pages between the first tokens and the windows may be gone, and their entries hold
+ * anything.  What a row attends to has to be finite for the row's result to be; a NaN or an
+ * infinity among the keys or values that the call reads may reach any row of its sequence.
+ */
+#define MEDHA_OUT_FP32 0
+#define MEDHA_OUT_BF16 1
+int medha_chunked_prefill_attn_fp8(const void* q, const medha_kv_cache_fp8* kv,
+                                   const int32_t* page_table, const int64_t* page_table_offs,
+                                   const int32_t* prefix_len, const int32_t* chunk_len,
+                                   int32_t batch, int32_t num_q_heads, float softmax_scale,
+                                   int32_t window, int32_t sinks, int32_t out_type, void* out,
+                                   float* lse, void* workspace, size_t workspace_bytes,
+                                   void* hip_stream);
+
+size_t medha_chunked_prefill_fp8_workspace_bytes(const int32_t* prefix_len,
+                                                 const int32_t* chunk_len, int32_t batch,
+                                                 int32_t num_q_heads, int32_t num_kv_heads,
+                                                 int32_t head_dim, int32_t window, int32_t sinks);
+
+/*
+ * The same attention behind a window (>= 1) over the bf16 cache, for models whose layers see the
+ * last tokens and a sequence's first ones only: a chunk costs its rows times the window, whatever
+ * its prefix, and pages behind the windows can be given back.
+ */
+int medha_window_attn(const void* q, const medha_kv_cache* kv, const int32_t* page_table,
+                      const int64_t* page_table_offs, const int32_t* prefix_len,
+                      const int32_t* chunk_len, int32_t batch, int32_t num_q_heads,
+                      float softmax_scale, int32_t window, int32_t sinks, int32_t out_type,
+                      void* out, float* lse, void* workspace, size_t workspace_bytes,
+                      void* hip_stream);
+
+size_t medha_window_workspace_bytes(const int32_t* prefix_len, const int32_t* chunk_len,
+                                    int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                    int32_t head_dim, int32_t window, int32_t sinks);
+
+/*
  * Introspection of the launch plan (host only; needs no GPU).  How the library
  * would lay a chunked-prefill batch out over workgroups on a device with
  * num_cus compute units (0 = the current device, or 256 if there is none):

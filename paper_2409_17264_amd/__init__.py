@@ -9,7 +9,9 @@ from .binding import (  # noqa: F401
     chunk_partial_attn,
     chunk_partial_workspace_bytes,
     chunked_prefill_attn,
+    chunked_prefill_attn_fp8,
     chunked_prefill_attn_noalloc,
+    chunked_prefill_fp8_workspace_bytes,
     chunked_prefill_workspace_bytes,
     decode_partial_attn,
     decode_partial_workspace_bytes,
@@ -22,4 +24,6 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
     lse_merge,
+    window_attn,
+    window_workspace_bytes,
 )

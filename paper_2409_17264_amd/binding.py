@@ -8,6 +8,7 @@ torch's current stream and returns without synchronising.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 import warnings
 from typing import Optional, Sequence
@@ -35,6 +36,10 @@ EXPORTS = (
     "medha_kv_append",
     "medha_kv_append_fp8",
     "medha_kv_read_fp8",
+    "medha_chunked_prefill_attn_fp8",
+    "medha_chunked_prefill_fp8_workspace_bytes",
+    "medha_window_attn",
+    "medha_window_workspace_bytes",
     "medha_describe_plan",
     "medha_describe_plan_slot",
     "medha_describe_slot",
@@ -110,6 +115,14 @@ def load_library():
     lib.medha_kv_append_fp8.argtypes = [vp, vp, ctypes.POINTER(_KvCacheFp8), vp, vp, vp, vp, i32, vp]
     lib.medha_kv_read_fp8.restype = ctypes.c_int
     lib.medha_kv_read_fp8.argtypes = [ctypes.POINTER(_KvCacheFp8), vp, vp, vp, vp, i32, vp, vp, vp]
+    for name, cache in (("chunked_prefill_attn_fp8", _KvCacheFp8), ("window_attn", _KvCache)):
+        attn = getattr(lib, "medha_" + name)
+        attn.restype = ctypes.c_int
+        attn.argtypes = [vp, ctypes.POINTER(cache), vp, vp, vp, vp, i32, i32, f32, i32, i32, i32, vp,
+                         vp, vp, sz, vp]
+    for query in (lib.medha_chunked_prefill_fp8_workspace_bytes, lib.medha_window_workspace_bytes):
+        query.restype = sz
+        query.argtypes = [vp, vp, i32, i32, i32, i32, i32, i32]
     lib.medha_describe_plan.restype = ctypes.c_int
     lib.medha_describe_plan.argtypes = [vp, vp, i32, i32, i32, i32, i32, ctypes.POINTER(PlanEntry),
                                         ctypes.POINTER(i32), ctypes.POINTER(i32),
@@ -138,7 +151,7 @@ class _LongWay:
         return None
 
     chunked_prefill_attn = decode_partial_attn = chunk_partial_attn = lse_merge = kv_append = _none
-    kv_append_fp8 = kv_read_fp8 = _none
+    kv_append_fp8 = kv_read_fp8 = window_attn = chunked_prefill_attn_fp8 = _none
 
 
 def _extension_module(lib):
@@ -162,7 +175,9 @@ def _extension_module(lib):
         "chunked_prefill_attn", "chunked_prefill_attn_alloc", "decode_partial_attn",
         "decode_partial_workspace_bytes", "chunk_partial_attn", "chunk_partial_workspace_bytes",
         "lse_merge", "kv_append"))
-    _marshal.bind_fp8(torch.cuda.current_device, *addresses("kv_append_fp8", "kv_read_fp8"))
+    _marshal.bind_fp8(torch.cuda.current_device, *addresses(
+        "kv_append_fp8", "kv_read_fp8", "window_attn", "window_attn_alloc",
+        "chunked_prefill_attn_fp8", "chunked_prefill_attn_fp8_alloc"))
     return _marshal
 
 
@@ -552,3 +567,85 @@ def kv_read_fp8(k_pool: torch.Tensor, v_pool: torch.Tensor, kv_scale: torch.Tens
         _check(lib.medha_kv_read_fp8(ctypes.byref(kv), _dp(page_table), _hp(offs), _hp(fst),
                                      _hp(cnt), len(fst), _dp(k_out), _dp(v_out), _stream()))
     return k_out, v_out
+
+
+def chunked_prefill_fp8_workspace_bytes(prefix_len, chunk_len, num_q_heads: int, num_kv_heads: int,
+                                        head_dim: int, window: int = 0, sinks: int = 0) -> int:
+    pre, chk = _host(prefix_len, np.int32), _host(chunk_len, np.int32)
+    return int(load_library().medha_chunked_prefill_fp8_workspace_bytes(
+        _hp(pre), _hp(chk), len(pre), num_q_heads, num_kv_heads, head_dim, window, sinks))
+
+
+def window_workspace_bytes(prefix_len, chunk_len, num_q_heads: int, num_kv_heads: int,
+                           head_dim: int, window: int, sinks: int = 0) -> int:
+    pre, chk = _host(prefix_len, np.int32), _host(chunk_len, np.int32)
+    return int(load_library().medha_window_workspace_bytes(
+        _hp(pre), _hp(chk), len(pre), num_q_heads, num_kv_heads, head_dim, window, sinks))
+
+
+def _windowed(call, query, kv, q, page_table, page_table_offs, prefix_len, chunk_len, softmax_scale,
+              window, sinks, out, lse, workspace):
+    """The long way of the two calls below."""
+    assert q.dtype == torch.bfloat16 and q.is_contiguous() and q.dim() == 3
+    _same_device(q)
+    tokens, h_q, d = q.shape
+    assert d == kv.head_dim
+    pre, chk = _host(prefix_len, np.int32), _host(chunk_len, np.int32)
+    offs = _pages(page_table, page_table_offs, len(pre))
+    assert len(chk) == len(pre) and _total(chk) == tokens
+    window, sinks = operator.index(window), operator.index(sinks)
+    assert -2 ** 31 <= min(window, sinks) and max(window, sinks) < 2 ** 31
+    if out is None:
+        out = torch.empty((tokens, h_q, d), dtype=torch.float32, device=q.device)
+    assert out.dtype in (torch.float32, torch.bfloat16)
+    assert out.is_contiguous() and out.shape == (tokens, h_q, d)
+    lse = _output(lse, (tokens, h_q), q.device)
+    if workspace is None:
+        workspace = _workspace(query(_hp(pre), _hp(chk), len(pre), h_q, kv.num_kv_heads, d, window,
+                                     sinks), q.device)
+    else:
+        _check_workspace(workspace)
+    _same_device(out, lse, workspace)
+    _check(call(_dp(q), ctypes.byref(kv), _dp(page_table), _hp(offs), _hp(pre), _hp(chk), len(pre),
+                h_q, float(softmax_scale), window, sinks, int(out.dtype == torch.bfloat16),
+                _dp(out), _dp(lse), _dp(workspace), workspace.numel(), _stream()))
+    return out, lse
+
+
+def chunked_prefill_attn_fp8(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+                             kv_scale: torch.Tensor, page_table: torch.Tensor, page_table_offs,
+                             prefix_len, chunk_len, softmax_scale: float, window: int = 0,
+                             sinks: int = 0, out: Optional[torch.Tensor] = None,
+                             lse: Optional[torch.Tensor] = None,
+                             workspace: Optional[torch.Tensor] = None):
+    """chunked_prefill_attn over the 8-bit cache (see kv_append_fp8), behind a window if `window` is
+    not 0 (see window_attn).  Returns (out, lse); `out` may be given in bf16 and is fp32 if not."""
+    lib = load_library()
+    done = _NATIVE.chunked_prefill_attn_fp8(q, k_pool, v_pool, kv_scale, page_table,
+                                            page_table_offs, prefix_len, chunk_len, softmax_scale,
+                                            window, sinks, out, lse, workspace)
+    if done is not None:
+        return done
+    return _windowed(lib.medha_chunked_prefill_attn_fp8,
+                     lib.medha_chunked_prefill_fp8_workspace_bytes,
+                     _kv_fp8(k_pool, v_pool, kv_scale), q, page_table, page_table_offs, prefix_len,
+                     chunk_len, softmax_scale, window, sinks, out, lse, workspace)
+
+
+def window_attn(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+                page_table: torch.Tensor, page_table_offs, prefix_len, chunk_len,
+                softmax_scale: float, window: int, sinks: int = 0,
+                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None):
+    """chunked_prefill_attn in which the row at position p attends to keys t <= p with
+    t > p - window or t < sinks only; pages that no row needs may be gone, their table entries are
+    not used.  Returns (out, lse); `out` may be given in bf16 and is fp32 if not."""
+    lib = load_library()
+    done = _NATIVE.window_attn(q, k_pool, v_pool, page_table, page_table_offs, prefix_len, chunk_len,
+                               softmax_scale, window, sinks, out, lse, workspace)
+    if done is not None:
+        return done
+    _same_device(k_pool, v_pool)
+    return _windowed(lib.medha_window_attn, lib.medha_window_workspace_bytes, _kv(k_pool, v_pool), q,
+                     page_table, page_table_offs, prefix_len, chunk_len, softmax_scale, window, sinks,
+                     out, lse, workspace)

@@ -139,7 +139,7 @@ decode_kernel(const AttnArgs args) {
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
   const int kv_total = sd.kv_len;  // keys that exist
-  rb.limit = min(sd.prefix_len + tok, kv_total - 1);
+  rb.mask.limit = min(sd.prefix_len + tok, kv_total - 1);
   {
     const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
     const __bf16* qp = args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D + half * 8;

@@ -39,6 +39,10 @@ struct Library {
   decltype(&medha_kv_append) append = nullptr;
   decltype(&medha_kv_append_fp8) append_fp8 = nullptr;
   decltype(&medha_kv_read_fp8) read_fp8 = nullptr;
+  decltype(&medha_window_attn) window = nullptr;
+  decltype(&medha_window_attn_alloc) window_alloc = nullptr;
+  decltype(&medha_chunked_prefill_attn_fp8) fp8 = nullptr;
+  decltype(&medha_chunked_prefill_attn_fp8_alloc) fp8_alloc = nullptr;
   PyObject* stream = nullptr;
   PyObject* device = nullptr;  // index of the current one
   PyObject* check = nullptr;  // raises an error code of the library's
@@ -529,6 +533,91 @@ PyObject* kv_read_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// A Python integer that an int32 holds.
+bool integer(PyObject* o, int32_t& x) {
+  if (!PyLong_CheckExact(o)) return false;
+  int overflow;
+  const long long v = PyLong_AsLongLongAndOverflow(o, &overflow);
+  x = (int32_t)v;
+  return overflow == 0 && v == x;
+}
+
+// An attention output in fp32 or, where the caller's is, in bf16.
+bool output_of_type(PyObject* o, at::IntArrayRef sizes, const at::Tensor& like, at::Tensor& t,
+                    int32_t& type) {
+  const at::Tensor* given = o == Py_None ? nullptr : tensor(o);
+  const bool bf16 = given != nullptr && given->scalar_type() == at::kBFloat16;
+  type = bf16 ? MEDHA_OUT_BF16 : MEDHA_OUT_FP32;
+  return output(o, sizes, like, t, bf16 ? at::kBFloat16 : at::kFloat);
+}
+
+// The calls with a window; `from`: place of the page table among the arguments, behind q, the pools
+// and what else the cache has.
+// (.., page_table, offs, prefix_len, chunk_len, scale, window, sinks, out, lse, workspace)
+template <class Cache, class Call, class CallAlloc>
+PyObject* windowed(PyObject* const* a, const Cache& kv, int from, Call call, CallAlloc call_alloc) {
+  const at::Tensor *q, *table;
+  HostArray<int64_t> offs;
+  HostArray<int32_t> pre, chk;
+  float scale;
+  int32_t window, sinks, type;
+  void* stream;
+  PyObject* const* b = a + from;
+  if (!pre.take(b[2]) || !chk.take(b[3]) || !offs.take(b[1]) ||
+      !device_array(q = tensor(a[0]), at::kBFloat16, 3) || q->size(2) != kv.head_dim ||
+      chk.size() != pre.size() || !pages(table = tensor(b[0]), offs, pre.size()) ||
+      total(chk) != q->size(0) || q->size(1) > std::numeric_limits<int32_t>::max() ||
+      !integer(b[5], window) || !integer(b[6], sinks))
+    return nullptr;
+  at::Tensor out, lse, given;
+  const c10::DeviceIndex device = q->get_device();
+  if (!output_of_type(b[7], q->sizes(), *q, out, type) ||
+      !output(b[8], q->sizes().slice(0, 2), *q, lse) || !room(b[9], given) ||
+      !on_device(tensor(a[1]), device) || !on_device(tensor(a[2]), device) ||
+      !on_device(table, device) || !on_device(&out, device) || !on_device(&lse, device) ||
+      (given.defined() && !on_device(&given, device)) || !number(b[4], scale) ||
+      !current_stream_of(device, stream))
+    return nullptr;
+  Workspace ws{{}, q->options(), nullptr};
+  const void* qp = q->data_ptr();
+  const int32_t* tp = static_cast<const int32_t*>(table->data_ptr());
+  void* op = out.data_ptr();
+  float* lp = static_cast<float*>(lse.data_ptr());
+  void* wp = given.defined() ? given.data_ptr() : nullptr;
+  const int32_t batch = (int32_t)pre.size(), h_q = (int32_t)q->size(1);
+  int rc;
+  {
+    Unlocked unlocked;
+    rc = given.defined()
+             ? call(qp, &kv, tp, offs.data(), pre.data(), chk.data(), batch, h_q, scale, window,
+                    sinks, type, op, lp, wp, (size_t)given.numel(), stream)
+             : call_alloc(qp, &kv, tp, offs.data(), pre.data(), chk.data(), batch, h_q, scale,
+                          window, sinks, type, op, lp, allocate, &ws, stream);
+  }
+  if (ws.error) std::rethrow_exception(ws.error);
+  return made(rc) ? pair(b[7], out, b[8], lse) : nullptr;
+}
+
+// (q, k_pool, v_pool, page_table, offs, prefix_len, chunk_len, scale, window, sinks, out, lse,
+// workspace)
+PyObject* window_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return ordinary([&]() -> PyObject* {
+    medha_kv_cache kv;
+    if (n != 13 || !cache(a[1], a[2], kv)) return nullptr;
+    return windowed(a, kv, 3, lib.window, lib.window_alloc);
+  });
+}
+
+// (q, k_pool, v_pool, kv_scale, page_table, offs, prefix_len, chunk_len, scale, window, sinks, out,
+// lse, workspace)
+PyObject* chunked_prefill_attn_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return ordinary([&]() -> PyObject* {
+    medha_kv_cache_fp8 kv;
+    if (n != 14 || !cache_fp8(a[1], a[2], a[3], kv)) return nullptr;
+    return windowed(a, kv, 4, lib.fp8, lib.fp8_alloc);
+  });
+}
+
 // Reads entry points' addresses; false with a Python error.
 template <int kEntries>
 bool addresses(PyObject* const* a, void* (&p)[kEntries]) {
@@ -560,7 +649,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // bind_fp8(function for the current device's index, entry points' addresses in the order below)
 PyObject* bind_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  constexpr int kEntries = 2;
+  constexpr int kEntries = 6;
   if (n != 1 + kEntries) {
     PyErr_Format(PyExc_TypeError, "bind_fp8() takes %d arguments", 1 + kEntries);
     return nullptr;
@@ -569,6 +658,10 @@ PyObject* bind_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!addresses(a + 1, p)) return nullptr;
   lib.append_fp8 = reinterpret_cast<decltype(lib.append_fp8)>(p[0]);
   lib.read_fp8 = reinterpret_cast<decltype(lib.read_fp8)>(p[1]);
+  lib.window = reinterpret_cast<decltype(lib.window)>(p[2]);
+  lib.window_alloc = reinterpret_cast<decltype(lib.window_alloc)>(p[3]);
+  lib.fp8 = reinterpret_cast<decltype(lib.fp8)>(p[4]);
+  lib.fp8_alloc = reinterpret_cast<decltype(lib.fp8_alloc)>(p[5]);
   Py_XSETREF(lib.device, Py_NewRef(a[0]));
   Py_RETURN_NONE;
 }
@@ -576,7 +669,8 @@ PyObject* bind_fp8(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(bind), CALL(bind_fp8), CALL(chunked_prefill_attn), CALL(decode_partial_attn),
                          CALL(chunk_partial_attn), CALL(lse_merge), CALL(kv_append),
-                         CALL(kv_append_fp8), CALL(kv_read_fp8),
+                         CALL(kv_append_fp8), CALL(kv_read_fp8), CALL(window_attn),
+                         CALL(chunked_prefill_attn_fp8),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 

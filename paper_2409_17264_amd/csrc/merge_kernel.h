@@ -19,7 +19,9 @@ struct MergeState {
 // 4 head-dim elements d4*4 .. +3.  Partial s of the row sits at row index base + s * stride
 // of the partial arrays.  The partials are taken kBatch at a time with all loads of a batch in
 // flight together (the merge is a chain of memory latencies, nothing else), and batches are
-// folded with the same online rescaling the attention kernels use.
+// folded with the same online rescaling the attention kernels use.  kNan: a partial whose LSE is
+// NaN makes the result NaN; otherwise it weighs zero.
+template <bool kNan = false>
 __device__ __forceinline__ void fold_partials(const float* __restrict__ part_o,
                                               const float* __restrict__ part_lse, int n_split,
                                               int s_first, int s_step, int64_t base,
@@ -42,14 +44,15 @@ __device__ __forceinline__ void fold_partials(const float* __restrict__ part_o,
       if (s0 + i * s_step >= n_split) ls[i] = -INFINITY;
       top = fmaxf(top, ls[i]);
     }
-    if (top == -INFINITY) continue;  // nothing but empty shards so far
+    if (top == -INFINITY && !kNan) continue;  // nothing but empty shards so far
+    if (kNan) top = fmaxf(top, -__FLT_MAX__);     // (the same, and NaN stay what they are)
     const float keep = fast_exp2((st.big - top) * kLog2e);  // 0 while big is -inf
     st.wsum *= keep;
     st.acc *= keep;
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
       const float w = fast_exp2((ls[i] - top) * kLog2e);
-      if (w > 0.f) {  // an empty shard's O is never read into the sum
+      if (kNan ? w != 0.f : w > 0.f) {  // an empty shard's O is never read into the sum
         st.wsum += w;
         st.acc += ov[i] * w;
       }
@@ -58,23 +61,32 @@ __device__ __forceinline__ void fold_partials(const float* __restrict__ part_o,
   }
 }
 
+__device__ __forceinline__ void store4(float* to, const f32x4& v) {
+  *reinterpret_cast<f32x4*>(to) = v;
+}
+__device__ __forceinline__ void store4(__bf16* to, const f32x4& v) {
+  *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(v, bf16x4);
+}
+
+template <bool kNan = false, class Out>
 __device__ __forceinline__ void finish_merge(const MergeState& st, int d4,
-                                             float* __restrict__ out_row,
+                                             Out* __restrict__ out_row,
                                              float* __restrict__ lse_out) {
-  const float inv = st.wsum > 0.f ? 1.f / st.wsum : 0.f;
-  *reinterpret_cast<f32x4*>(out_row + d4 * 4) = st.acc * inv;
-  if (d4 == 0) *lse_out = st.wsum > 0.f ? st.big + fast_log2(st.wsum) * kLn2 : -INFINITY;
+  const bool some = kNan ? st.wsum != 0.f : st.wsum > 0.f;
+  store4(out_row + d4 * 4, st.acc * (some ? 1.f / st.wsum : 0.f));
+  if (d4 == 0) *lse_out = some ? st.big + fast_log2(st.wsum) * kLn2 : -INFINITY;
 }
 
 // One thread owns 4 consecutive head-dim elements of one (row, head) and all its partials.
+template <bool kNan = false, class Out>
 __device__ __forceinline__ void merge_one(const float* __restrict__ part_o,
                                           const float* __restrict__ part_lse, int n_split,
                                           int64_t base, int64_t stride, int h_q, int head, int d,
-                                          int d4, float* __restrict__ out_row,
+                                          int d4, Out* __restrict__ out_row,
                                           float* __restrict__ lse_out) {
   MergeState st;
-  fold_partials(part_o, part_lse, n_split, 0, 1, base, stride, h_q, head, d, d4, st);
-  finish_merge(st, d4, out_row, lse_out);
+  fold_partials<kNan>(part_o, part_lse, n_split, 0, 1, base, stride, h_q, head, d, d4, st);
+  finish_merge<kNan>(st, d4, out_row, lse_out);
 }
 
 // Public merge: uniform split count, partials [n_split][rows][h_q][d].
@@ -95,7 +107,8 @@ static __global__ void __launch_bounds__(kThreads) lse_merge_kernel(
 // Merge of the library's own split-KV partials, laid out per sequence:
 // partial s of token j of a sequence is row  part_row + s * chunk_len + j.
 // Sequences that were not split wrote their result directly and are skipped.
-template <int D>
+// Out: type of the result, float or __bf16 (args.out points at it).
+template <int D, class Out = float, bool kNan = false>
 __global__ void __launch_bounds__(kThreads) split_merge_kernel(const MergeArgs args) {
   constexpr int per_row = D / 4;
   const SeqDesc* descs = args.inline_descs;
@@ -112,8 +125,8 @@ __global__ void __launch_bounds__(kThreads) split_merge_kernel(const MergeArgs a
   if (sd.n_split == 1) return;
   const int j = row - sd.row_rank;
   const int64_t orow = ((int64_t)sd.out_row + j) * args.h_q + head;
-  merge_one(args.part_o, args.part_lse, sd.n_split, (int64_t)sd.part_row + j, sd.chunk_len,
-            args.h_q, head, D, d4, args.out + orow * D, args.lse + orow);
+  merge_one<kNan>(args.part_o, args.part_lse, sd.n_split, (int64_t)sd.part_row + j, sd.chunk_len,
+            args.h_q, head, D, d4, reinterpret_cast<Out*>(args.out) + orow * D, args.lse + orow);
 }
 
 // The same merge for launches with many KV ranges per row (small chunks against a long
@@ -121,7 +134,7 @@ __global__ void __launch_bounds__(kThreads) split_merge_kernel(const MergeArgs a
 // D/4 column groups x 256/(D/4) lanes, lane l folds ranges l, l + lanes, ..., and the
 // lanes' states are combined through LDS.  The chain of dependent memory latencies is
 // `lanes` times shorter than with one thread per column group.
-template <int D>
+template <int D, class Out = float, bool kNan = false>
 __global__ void __launch_bounds__(kThreads) split_merge_wide_kernel(const MergeArgs args) {
   constexpr int per_row = D / 4;
   constexpr int lanes = kThreads / per_row;
@@ -136,7 +149,7 @@ __global__ void __launch_bounds__(kThreads) split_merge_wide_kernel(const MergeA
   const int d4 = threadIdx.x % per_row;
   const int lane = threadIdx.x / per_row;
   MergeState st;
-  fold_partials(args.part_o, args.part_lse, sd.n_split, lane, lanes, (int64_t)sd.part_row + j,
+  fold_partials<kNan>(args.part_o, args.part_lse, sd.n_split, lane, lanes, (int64_t)sd.part_row + j,
                 sd.chunk_len, args.h_q, head, D, d4, st);
   sm_acc[lane][d4] = st.acc;
   if (d4 == 0) {
@@ -152,14 +165,14 @@ __global__ void __launch_bounds__(kThreads) split_merge_wide_kernel(const MergeA
 #pragma unroll
     for (int l = 0; l < lanes; ++l) {
       const float w = fast_exp2((sm_big[l] - all.big) * kLog2e);  // 0 for a lane that saw nothing
-      if (sm_wsum[l] > 0.f) {
+      if (kNan ? sm_wsum[l] != 0.f : sm_wsum[l] > 0.f) {
         all.wsum += w * sm_wsum[l];
         all.acc += sm_acc[l][d4] * w;
       }
     }
   }
   const int64_t orow = ((int64_t)sd.out_row + j) * args.h_q + head;
-  finish_merge(all, d4, args.out + orow * D, args.lse + orow);
+  finish_merge<kNan>(all, d4, reinterpret_cast<Out*>(args.out) + orow * D, args.lse + orow);
 }
 
 }  // namespace medha

@@ -195,7 +195,13 @@ __device__ __forceinline__ void static_for(F& f) {
   static_for_impl(std::make_integer_sequence<int, N>{}, f);
 }
 
-template <int D>
+// Which keys a row sees: those up to its limit.
+struct CausalMask {
+  int limit;  // last visible key index of the lane's row
+  __device__ __forceinline__ bool sees(int t) const { return t <= limit; }
+};
+
+template <int D, class Mask = CausalMask>
 struct RowBlock {
   static constexpr int kSlices = D / 16;
   static constexpr int kDBlocks = D / 32;
@@ -203,7 +209,7 @@ struct RowBlock {
   f32x16 o[kDBlocks];
   float m;        // reference point of the exponentials (log2 domain), see update_reference()
   float l;        // kSpecShare * (this lane's share of the running sum), see add_to_sum()
-  int limit;      // last visible key index of the lane's row
+  Mask mask;      // of the lane's row
   float scale_log2;
   // per-lane LDS byte offsets of the operand reads inside a stage
   int k_off[kSlices];
@@ -335,7 +341,7 @@ struct RowBlock {
       for (int e = 0; e < 16; ++e) {
         if (MASK) {
           const int t = key0 + kb * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[kb][e] = (t <= limit) ? s[kb][e] : -INFINITY;
+          s[kb][e] = mask.sees(t) ? s[kb][e] : -INFINITY;
         }
         mx = fmaxf(mx, s[kb][e]);
       }
@@ -509,7 +515,7 @@ struct RowBlock {
         for (int f = i * per; f < (i + 1) * per; ++f) {
           if (MASK) {
             const int t = key0 + (f >> 4) * 32 + 8 * ((f & 15) >> 2) + 4 * half + (f & 3);
-            sc[f >> 4][f & 15] = (t <= limit) ? sc[f >> 4][f & 15] : -INFINITY;
+            sc[f >> 4][f & 15] = mask.sees(t) ? sc[f >> 4][f & 15] : -INFINITY;
           }
           mx = fmaxf(mx, sc[f >> 4][f & 15]);
         }
@@ -824,7 +830,7 @@ __global__ void __launch_bounds__(512) prefill_kernel(const AttnArgs args) {
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
   const int kv_total = sd.kv_len;  // keys that exist
-  rb.limit = min(sd.prefix_len + tok, kv_total - 1);
+  rb.mask.limit = min(sd.prefix_len + tok, kv_total - 1);
   {
     // a negative scale is folded into the sign of Q (exact), so the kernel's scale is >= 0
     const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;

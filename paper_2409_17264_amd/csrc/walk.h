@@ -1,0 +1,53 @@
+// Which keys the rows of a workgroup see under a sliding window with first tokens that stay
+// visible, and the order in which their tiles are walked.  Host and device.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace medha {
+
+// The row at position p sees key t if t <= p and (t > p - keys or t < sinks).
+struct Window {
+  int32_t keys = INT32_MAX;  // INT32_MAX: no window
+  int32_t sinks = 0;
+};
+
+// The tiles of `tile_keys` keys that rows at positions [p_a, p_b] see, as one row of n indexes.
+// Their windows reach keys [lo, end); before lo they see keys [0, first).  Softmax attention does
+// not care for the order of its keys, so the tiles that every row sees in full come first
+// (n_full of them, which need no mask), behind them the other tiles up to the rows' own, the first
+// tokens' tiles and the left edge of the windows:
+//     [u0, w1)  [0, s1)  [w0, u0)
+struct KeyWalk {
+  int32_t lo, end, first;
+  int32_t w0, w1, u0, s1;
+  int32_t n, n_full;
+
+  __host__ __device__ __forceinline__ int tile(int i) const {
+    const int from_u0 = u0 + i, rest = i - (w1 - u0);
+    return rest < 0 ? from_u0 : rest < s1 ? rest : w0 + rest - s1;
+  }
+};
+
+// 0 <= p_a <= p_b < 2^31 - 1.
+__host__ __device__ inline KeyWalk make_walk(int32_t p_a, int32_t p_b, const Window& win,
+                                             int32_t tile_keys) {
+  const auto at_least_0 = [](int32_t x) { return x > 0 ? x : 0; };
+  KeyWalk k;
+  k.lo = at_least_0(p_a - win.keys + 1);
+  k.end = p_b + 1;
+  k.first = win.sinks < k.lo ? win.sinks : k.lo;
+  k.w0 = k.lo / tile_keys;
+  k.w1 = (k.end - 1) / tile_keys + 1;
+  const int32_t s1 = k.first > 0 ? (k.first - 1) / tile_keys + 1 : 0;
+  k.s1 = s1 < k.w0 ? s1 : k.w0;
+  const int32_t all_see = at_least_0(p_b - win.keys + 1);  // from here on every row sees, up to p_a
+  const int32_t u0 = all_see > 0 ? (all_see - 1) / tile_keys + 1 : 0, u1 = (p_a + 1) / tile_keys;
+  k.n_full = u1 > u0 ? u1 - u0 : 0;
+  k.u0 = k.n_full > 0 ? u0 : k.w0;
+  k.n = k.w1 - k.w0 + k.s1;
+  return k;
+}
+
+}  // namespace medha

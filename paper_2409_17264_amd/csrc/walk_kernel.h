@@ -1,0 +1,423 @@
+// Key-split attention over a window of a paged cache, in bf16 or in 8 bits.
+//
+// A workgroup owns 32 query rows (token, head-in-group) of one KV head and a range of their walk
+// (KeyWalk, in blocks of 32 keys); its 4 wavefronts take the range's blocks in turn, each with its
+// own online-softmax state, and the four states are combined through LDS at the end.  Each
+// wavefront streams its blocks HBM -> LDS with asynchronous 16-byte loads into a private ring, so
+// the loop has no workgroup barrier.
+//
+// Only keys that some row of the workgroup sees are read: what lies between the first tokens and
+// the windows stands in for a key that is seen, and is masked.  The pages there may be gone.
+#pragma once
+
+#include <type_traits>
+
+#include "common.h"
+#include "decode_kernel.h"
+#include "fp8_cache_kernel.h"
+#include "merge_kernel.h"
+#include "prefill_kernel.h"
+#include "walk.h"
+
+namespace medha {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct WalkArgs {
+  const __bf16* q;
+  const char* k_pool;
+  const char* v_pool;
+  const uint8_t* scale;  // 8-bit cache only
+  const int32_t* page_table;
+  void* out;             // fp32, or bf16 if out_bf16
+  float* lse;
+  float* part_o;
+  float* part_lse;
+  int32_t n_seq;
+  int32_t h_q;
+  int32_t h_kv;
+  float scale_log2;
+  Window window;
+  int32_t out_bf16;
+  int32_t reserved;
+  SeqDesc inline_descs[kMaxInlineSeq];
+};
+static_assert(sizeof(WalkArgs) <= 4096, "kernel argument block too large");
+
+struct WindowMask {
+  int limit;  // the row's position
+  int lo;     // first key of its window
+  int sinks;
+  __device__ __forceinline__ bool sees(int t) const {
+    return (t <= limit) & ((t >= lo) | (t < sinks));
+  }
+  __device__ __forceinline__ void set(int position, const Window& w) {
+    limit = position;
+    lo = position - w.keys + 1;
+    sinks = w.sinks;
+  }
+};
+
+// Where the 16 keys of one page's worth of a walk, from key g (a multiple of 16) on, are read from.
+struct PageRead {
+  int page_index;    // in the sequence's table (wave-uniform)
+  int g, lo, end, first;
+  bool sinks_only;   // the group ends before the windows begin, but holds first tokens
+  __device__ __forceinline__ PageRead(const KeyWalk& w, int group) {
+    g = group;
+    lo = w.lo;
+    end = w.end;
+    first = w.first;
+    const bool below = g + kPageSize <= lo;
+    sinks_only = below && g < first;
+    const int t = below && !sinks_only ? lo : min(g, end - 1);
+    page_index = t >> 4;
+  }
+  // Slot to read for key g + r: its own if some row sees it, that of a key that is seen otherwise.
+  __device__ __forceinline__ int slot(int r) const {
+    const int t = g + r;
+    const int near = sinks_only ? first - 1 : max(t, lo);
+    return min(t < first ? t : near, end - 1) & (kPageSize - 1);
+  }
+};
+
+__device__ __forceinline__ void async_load4(const void* gptr, uint32_t lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(lds_addr_uniform), "v"(gptr)
+               : "m0", "memory");
+}
+
+// ---------------------------------------------------------------- a block of 32 keys, bf16 cache
+
+template <int D>
+struct Bf16Block {
+  using G = DecodeGeom<D>;
+  using Rows = RowBlock<D, WindowMask>;
+  static constexpr int kBytes = G::kBlockBytes;   // ring stage
+  static constexpr int kScratchBytes = 0;         // per wavefront, beside the ring
+  static constexpr int kLoads = G::kLoadsPerBlock;
+
+  __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
+                                                bool valid, int half) {
+    const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+    for (int sl = 0; sl < Rows::kSlices; ++sl) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (valid) raw = *reinterpret_cast<const uint4*>(qp + sl * 16 + half * 8);
+      raw.x ^= flip; raw.y ^= flip; raw.z ^= flip; raw.w ^= flip;
+      rb.q[sl] = __builtin_bit_cast(bf16x8, raw);
+    }
+  }
+
+  __device__ static __forceinline__ void issue(const WalkArgs& args, ConstI32Ptr pt, const KeyWalk& w,
+                                               int key0, int kv_head, uint32_t stage, int lane) {
+    const int r_in = lane / G::kChunksPerRow, pos = lane % G::kChunksPerRow;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const PageRead pr(w, key0 + p * kPageSize);
+      const int page = pt[__builtin_amdgcn_readfirstlane(pr.page_index)];
+      const int64_t base = ((int64_t)page * args.h_kv + kv_head) * (kPageSize * D * 2);
+#pragma unroll
+      for (int j = 0; j < kPageSize / G::kRowsPerInstr; ++j) {
+        const int r = j * G::kRowsPerInstr + r_in, row = p * kPageSize + r;
+        const int64_t off = base + pr.slot(r) * (D * 2);
+        const uint32_t to = stage + (p * kPageSize + j * G::kRowsPerInstr) * (D * 2);
+        async_stream16<false>(args.k_pool + off + Swz<D>::k(row, pos) * 16, to);
+        async_stream16<false>(args.v_pool + off + Swz<D>::v(row, pos) * 16, to + G::kHalfBytes);
+      }
+    }
+  }
+
+  template <bool MASK>
+  __device__ static __forceinline__ void step(Rows& rb, const char* stage, char*, const KeyWalk&,
+                                              int key0, int lane) {
+    rb.template step<1, MASK>(stage, stage + G::kHalfBytes, key0, lane >> 5);
+  }
+};
+
+// ---------------------------------------------------------------- a block of 32 keys, 8-bit cache
+
+// 16-byte chunk of a row of D bytes, so that 16 rows read at one logical chunk hit all banks.
+template <int D>
+__device__ __forceinline__ int swz8(int row, int chunk) {
+  return D == 128 ? (chunk ^ ((row >> 1) & 7)) : (chunk ^ ((row >> 2) & 3));
+}
+
+// Rows of one wavefront against an 8-bit cache.  S^T = K Q^T takes the keys as they are, with their
+// scale byte as the matrix instruction's block scale.  Q is split into two e4m3 parts, q = hi + lo:
+// 4 significant bits each make the 8 of a bf16 number, so nothing of Q is lost (an element below
+// 2^-13 of its row's largest keeps 2^-21 of that).  Two instructions of 32x32x64 take as long as the
+// four of 32x32x16 that bf16 operands take, and no key has to be converted.
+template <int D>
+struct Rows8 : RowBlock<D, WindowMask> {
+  using Base = RowBlock<D, WindowMask>;
+  static constexpr int kParts = D / 64;
+  i32x8 hi[kParts], lo[kParts];
+  int hi_scale, lo_scale;
+
+  __device__ __forceinline__ void set_q(const uint4 (&raw)[D / 16]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) top = max(top, 128u * max_exponent(raw[i]));
+    const float both = max_halves(__builtin_bit_cast(float, top << 16));
+    hi_scale = max((int)(__builtin_bit_cast(uint32_t, both) >> 23) - 7, kLeastScaleByte);
+    lo_scale = hi_scale - 4;
+    const float s = __builtin_bit_cast(float, (uint32_t)hi_scale << 23);
+    const float inv = __builtin_bit_cast(float, (uint32_t)(254 - hi_scale) << 23);
+#pragma unroll
+    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {  // 4 elements each
+        const uint4 x = raw[part * 4 + w / 2];
+        const uint32_t a = w % 2 ? x.z : x.x, b = w % 2 ? x.w : x.y;
+        s16x2 h = {0, 0};
+        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, a), s, false);
+        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, b), s, true);
+        hi[part][w] = __builtin_bit_cast(int, h);
+        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi[part][w], false);
+        const f32x2 h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi[part][w], true);
+        int r = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (low(a) * inv - h0[0]),
+                                                16.f * (high(a) * inv - h0[1]), 0, false);
+        lo[part][w] = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (low(b) * inv - h1[0]),
+                                                      16.f * (high(b) * inv - h1[1]), r, true);
+      }
+  }
+
+  // k_lds: rows of D bytes, swizzled; scales: as the pool has them, [page][2][16].
+  template <int NKB>
+  __device__ __forceinline__ void qk(const char* k_lds, const char* scales, int lane,
+                                     f32x16 (&s)[NKB]) const {
+    const int col = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+      const int row = kb * 32 + col;
+      const int ks = (uint8_t)scales[(row >> 4) * kScaleBytesPerPage + (row & 15)];
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        const int c = part * 4 + half * 2;
+        const i32x4 a0 = *reinterpret_cast<const i32x4*>(k_lds + row * D + swz8<D>(row, c) * 16);
+        const i32x4 a1 = *reinterpret_cast<const i32x4*>(k_lds + row * D + swz8<D>(row, c + 1) * 16);
+        const i32x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
+        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, hi[part], s[kb], 0, 0, 0, ks, 0, hi_scale);
+        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, lo[part], s[kb], 0, 0, 0, ks, 0, lo_scale);
+      }
+    }
+  }
+
+ private:
+  static __device__ __forceinline__ float low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+  static __device__ __forceinline__ float high(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+  static __device__ __forceinline__ uint32_t max_exponent(uint4 x) {
+    uint32_t top = 0;
+    for (uint32_t w : {x.x, x.y, x.z, x.w}) top = max(top, max((w >> 7) & 0xffu, (w >> 23) & 0xffu));
+    return top;
+  }
+};
+
+template <int D>
+struct Fp8Block {
+  using Rows = Rows8<D>;
+  static constexpr int kHalfBytes = 32 * D;
+  static constexpr int kBytes = 2 * kHalfBytes + 256;   // K, V, and 64 lanes' worth of scale bytes
+  static constexpr int kScratchBytes = 32 * D * 2;      // the block's values in bf16
+  static constexpr int kChunksPerRow = D / 16;
+  static constexpr int kRowsPerInstr = 64 / kChunksPerRow;  // 8 or 16
+  static constexpr int kInstr = 32 / kRowsPerInstr;
+  static constexpr int kLoads = 2 * kInstr + 1;
+
+  __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
+                                                bool valid, int half) {
+    const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
+    uint4 raw[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {  // part i / 4: this half's 32 elements of 64
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (valid) raw[i] = *reinterpret_cast<const uint4*>(qp + (i / 4) * 64 + half * 32 + (i % 4) * 8);
+      raw[i].x ^= flip; raw[i].y ^= flip; raw[i].z ^= flip; raw[i].w ^= flip;
+    }
+    rb.set_q(raw);
+  }
+
+  __device__ static __forceinline__ void issue(const WalkArgs& args, ConstI32Ptr pt, const KeyWalk& w,
+                                               int key0, int kv_head, uint32_t stage, int lane) {
+    const int r_in = lane / kChunksPerRow, pos = lane % kChunksPerRow;
+    int64_t page_head[2];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const PageRead pr(w, key0 + p * kPageSize);
+      const int page = pt[__builtin_amdgcn_readfirstlane(pr.page_index)];
+      page_head[p] = (int64_t)page * args.h_kv + kv_head;
+#pragma unroll
+      for (int j = 0; j < kPageSize / kRowsPerInstr; ++j) {
+        const int r = j * kRowsPerInstr + r_in, row = p * kPageSize + r;
+        const int64_t off = page_head[p] * (kPageSize * D) + pr.slot(r) * D;
+        const uint32_t to = stage + (p * kPageSize + j * kRowsPerInstr) * D;
+        async_stream16<false>(args.k_pool + off + swz8<D>(row, pos) * 16, to);
+        async_stream16<false>(args.v_pool + off + pos * 16, to + kHalfBytes);
+      }
+    }
+    // (lanes 0-7 and 8-15 hold the two pages' 32 bytes, the others repeat them)
+    const int64_t ph = (lane & 8) ? page_head[1] : page_head[0];
+    async_load4(args.scale + ph * kScaleBytesPerPage + (lane & 7) * 4, stage + 2 * kHalfBytes);
+  }
+
+  template <bool MASK>
+  __device__ static __forceinline__ void step(Rows& rb, const char* stage, char* scratch,
+                                              const KeyWalk& w, int key0, int lane) {
+    const char* scales = stage + 2 * kHalfBytes;
+    // the values become bf16, exactly, where the transposing reads expect them
+    const int r_in = lane / kChunksPerRow, pos = lane % kChunksPerRow;
+#pragma unroll
+    for (int j = 0; j < kInstr; ++j) {
+      const int row = j * kRowsPerInstr + r_in;
+      int slot = row & 15;
+      if (MASK) slot = PageRead(w, key0 + (j * kRowsPerInstr & 16)).slot(slot);
+      const uint32_t byte = (uint8_t)scales[(row >> 4) * kScaleBytesPerPage + kPageSize + slot];
+      const uint4 raw = *reinterpret_cast<const uint4*>(stage + kHalfBytes + j * 1024 + lane * 16);
+      char* to = scratch + row * (D * 2);
+      *reinterpret_cast<uint4*>(to + Swz<D>::v(row, 2 * pos) * 16) =
+          dequantise8(make_uint2(raw.x, raw.y), byte);
+      *reinterpret_cast<uint4*>(to + Swz<D>::v(row, 2 * pos + 1) * 16) =
+          dequantise8(make_uint2(raw.z, raw.w), byte);
+    }
+    asm volatile("" ::: "memory");  // (one wavefront's LDS accesses stay in order)
+    f32x16 s[1];
+    rb.template qk<1>(stage, scales, lane, s);
+    bf16x8 vop[2][Rows::kDBlocks];
+    rb.read_v_slice(scratch, 0, vop[0]);
+    rb.read_v_slice(scratch, 1, vop[1]);
+    rb.template softmax_pv<1, MASK>(s, scratch, vop, key0, lane >> 5);
+    asm volatile("" ::: "memory");
+  }
+};
+
+// ---------------------------------------------------------------- the kernel
+
+// 4 elements of a result, `i` counted in elements.
+__device__ __forceinline__ void store_out(void* to, int64_t i, const f32x4& v, bool as_bf16) {
+  if (as_bf16)
+    store4(static_cast<__bf16*>(to) + i, v);
+  else
+    store4(static_cast<float*>(to) + i, v);
+}
+
+// (launched with 256 threads; the bound: see decode_kernel)
+template <int D, class Block, int STAGES>
+__global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs args) {
+  constexpr int kWaveBytes = STAGES * Block::kBytes + Block::kScratchBytes;
+  constexpr int kCombineBytes = kWaves * 32 * (D + 2) * 4;
+  __shared__ __attribute__((aligned(1024))) char
+      lds[kWaves * kWaveBytes > kCombineBytes ? kWaves * kWaveBytes : kCombineBytes];
+  using Rows = typename Block::Rows;
+
+  const SeqDesc* descs = args.inline_descs;
+  const int lane = threadIdx.x & 63;
+  const int seq = find_seq_slot(descs, args.n_seq, blockIdx.x);
+  const SeqDesc sd = uniform(descs[seq]);
+  const KeySplitItem it =
+      key_split_item(sd, blockIdx.x - sd.work_start, args.h_kv * sd.n_row_tiles);
+  const int split = it.split;
+  const int kv_head = it.kv_head / sd.n_row_tiles, row0 = it.kv_head % sd.n_row_tiles * 32;
+
+  const int gqa = args.h_q / args.h_kv;
+  const int n_rows = min(32, sd.chunk_len * gqa - row0);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+
+  Rows rb;
+  rb.init(fabsf(args.scale_log2), lane);
+  const bool valid = col < n_rows;
+  const int rr = row0 + (valid ? col : n_rows - 1);
+  const int tok = rr / gqa;
+  const int hq = kv_head * gqa + rr % gqa;
+  rb.mask.set(sd.prefix_len + tok, args.window);
+  Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
+
+  const KeyWalk walk = make_walk(sd.prefix_len + row0 / gqa, sd.prefix_len + (row0 + n_rows - 1) / gqa,
+                                 args.window, 32);
+  const int b_begin = split * sd.tiles_per_split * kWaves;
+  const int b_end = min(walk.n, b_begin + sd.tiles_per_split * kWaves);
+  ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
+  char* ring = lds + wave * kWaveBytes;
+  char* scratch = ring + STAGES * Block::kBytes;
+  const uint32_t ring_lds = lds_address(lds) + wave * kWaveBytes;
+  auto issue = [&](int b, int st) {
+    Block::issue(args, pt, walk, walk.tile(b) * 32, kv_head, ring_lds + st * Block::kBytes, lane);
+  };
+  if (b_begin + wave < b_end) issue(b_begin + wave, 0);
+  int st = 0;
+  for (int b = b_begin + wave; b < b_end; b += kWaves, st ^= 1) {
+    if (b + kWaves < b_end) {
+      issue(b + kWaves, st ^ 1);
+      wait_vmcnt<Block::kLoads>();  // the younger block may still fly
+    } else {
+      wait_vmcnt<0>();
+    }
+    const char* stage = ring + st * Block::kBytes;
+    if (b < walk.n_full)
+      Block::template step<false>(rb, stage, scratch, walk, walk.tile(b) * 32, lane);
+    else
+      Block::template step<true>(rb, stage, scratch, walk, walk.tile(b) * 32, lane);
+    // every LDS read of the stage has returned (its data fed the matrix cores)
+  }
+
+  // Combine the 4 wavefronts' (m, l, O) over their disjoint keys through LDS.
+  const bool direct = sd.n_split == 1;
+  void* o_base = direct ? args.out : args.part_o;
+  float* l_base = direct ? args.lse : args.part_lse;
+  const bool as_bf16 = direct && args.out_bf16;
+  const int64_t row_base =
+      direct ? (int64_t)sd.out_row : (int64_t)sd.part_row + (int64_t)split * sd.chunk_len;
+  __syncthreads();  // all rings are drained and read
+  float* sm_o = reinterpret_cast<float*>(lds);  // [wave][32][D]
+  float* sm_ml = sm_o + kWaves * 32 * D;        // [wave][32][2]
+  const float lt = rb.row_sum();
+  if (valid) {
+    float* op = sm_o + (wave * 32 + col) * D + 4 * half;
+#pragma unroll
+    for (int db = 0; db < Rows::kDBlocks; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = rb.o[db][4 * i + j];
+        *reinterpret_cast<f32x4*>(op + db * 32 + 8 * i) = v;
+      }
+    if (half == 0) {
+      sm_ml[(wave * 32 + col) * 2 + 0] = rb.m;
+      sm_ml[(wave * 32 + col) * 2 + 1] = lt;
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < n_rows * (D / 4); e += kThreads) {
+    const int rl = e / (D / 4), d4 = e % (D / 4);
+    float mw[kWaves], lw[kWaves], mm = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      mw[w] = sm_ml[(w * 32 + rl) * 2 + 0];
+      lw[w] = sm_ml[(w * 32 + rl) * 2 + 1];
+      mm = fmaxf(mm, mw[w]);
+    }
+    // (a wavefront without a key has the sum 0; a NaN among a row's keys reaches its result)
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float lt_all = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (lw[w] == 0.f) continue;
+      const float a = fast_exp2(mw[w] - mm);
+      lt_all += a * lw[w];
+      acc += *reinterpret_cast<const f32x4*>(sm_o + (w * 32 + rl) * D + d4 * 4) * a;
+    }
+    const float inv = lt_all != 0.f ? 1.f / lt_all : 0.f;
+    const int r = row0 + rl;
+    const int64_t orow = (row_base + r / gqa) * args.h_q + kv_head * gqa + r % gqa;
+    store_out(o_base, orow * D + d4 * 4, acc * inv, as_bf16);
+    if (d4 == 0) l_base[orow] = lt_all != 0.f ? (mm + fast_log2(lt_all)) * kLn2 : -INFINITY;
+  }
+}
+
+}  // namespace medha
