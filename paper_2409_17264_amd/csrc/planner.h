@@ -15,7 +15,8 @@ namespace medha {
 struct ModeShape {
   int rows_per_wg;  // query rows a workgroup owns
   int tile_keys;    // keys staged per loop iteration (the KV split granule)
-  Window window{};
+  Window window{};  // of the rows,
+  int gqa = 1;      // of which so many belong to a token (looked at behind a window)
 };
 
 struct LaunchPlan {
@@ -167,10 +168,10 @@ inline double makespan(std::vector<WalkGroup>& groups, int64_t machines, const W
 
 // Tiles of the longest walk of a sequence's row tiles: all its keys, or with a window at most the
 // tiles that a row tile's windows and the first tokens can touch.
-inline int64_t kv_tiles_of(const SeqDesc& sd, const ModeShape& sh, int gqa) {
+inline int64_t kv_tiles_of(const SeqDesc& sd, const ModeShape& sh) {
   const int64_t all = std::max<int64_t>(1, ceil_div((int64_t)sd.kv_len, sh.tile_keys));
   if (sd.kv_len <= sh.window.keys) return all;
-  const int64_t tokens = std::min<int64_t>(sd.chunk_len, (sh.rows_per_wg + gqa - 2) / gqa + 1);
+  const int64_t tokens = std::min<int64_t>(sd.chunk_len, (sh.rows_per_wg + sh.gqa - 2) / sh.gqa + 1);
   const int64_t reach = sh.window.keys + tokens - 1;  // keys from the first row's window to the last row
   return std::min(all, (reach - 1) / sh.tile_keys + 2 + ceil_div(sh.window.sinks, sh.tile_keys));
 }
@@ -193,9 +194,9 @@ inline bool uneven_walks(const SeqDesc& sd, const ModeShape& sh, int gqa) {
 }
 
 // KV ranges of a sequence when no range is longer than `steps` tiles nor shorter than min_tiles.
-inline void split_by_steps(const SeqDesc& sd, const ModeShape& sh, int gqa, int64_t steps,
-                           int min_tiles, int64_t& n_split, int64_t& tps) {
-  const int64_t kv_tiles = kv_tiles_of(sd, sh, gqa);
+inline void split_by_steps(const SeqDesc& sd, const ModeShape& sh, int64_t steps, int min_tiles,
+                           int64_t& n_split, int64_t& tps) {
+  const int64_t kv_tiles = kv_tiles_of(sd, sh);
   n_split = ceil_div(kv_tiles, steps);
   n_split = std::min(n_split, std::max<int64_t>(1, kv_tiles / min_tiles));
   n_split = std::max<int64_t>(1, n_split);
@@ -245,7 +246,7 @@ inline LaunchWalks launch_walks(const LaunchPlan& lp, int h_kv, int gqa) {
       lw.total_tiles += t * (hi - lo) * h_kv;
       if (t > 0) lw.busy += (hi - lo) * h_kv;
     }
-    const int64_t kv_tiles = kv_tiles_of(sd, lp.shape, gqa);
+    const int64_t kv_tiles = kv_tiles_of(sd, lp.shape);
     lw.unsplit += n_rt * h_kv;
     lw.key_tiles += n_rt * h_kv * kv_tiles;
     lw.longest = std::max(lw.longest, kv_tiles);
@@ -260,11 +261,11 @@ struct SplitSize {
   int64_t items;  // slots that are not idle
 };
 
-inline SplitSize split_size(const LaunchPlan& lp, int h_kv, int gqa, int64_t steps, int min_tiles) {
+inline SplitSize split_size(const LaunchPlan& lp, int h_kv, int64_t steps, int min_tiles) {
   SplitSize s{0, 0, 0};
   int64_t n_split, tps;
   for (const SeqDesc& sd : lp.descs) {
-    split_by_steps(sd, lp.shape, gqa, steps, min_tiles, n_split, tps);
+    split_by_steps(sd, lp.shape, steps, min_tiles, n_split, tps);
     const int64_t items = (int64_t)h_kv * sd.n_row_tiles * n_split;
     s.items += items;
     s.slots += kXcds * ceil_div(items, kXcds);
@@ -289,7 +290,7 @@ inline double even_us(const LaunchWalks& lw, int64_t steps, int num_cus, const W
 }
 
 // Estimated time of a row-split launch whose KV ranges are at most `steps` tiles long.
-inline double launch_us(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, int gqa, int num_cus,
+inline double launch_us(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, int num_cus,
                         const WalkCost& wc, int64_t steps, int min_tiles, int64_t row_bytes) {
   std::vector<WalkGroup> groups;
   groups.reserve(4 * lw.classes.size());
@@ -297,7 +298,7 @@ inline double launch_us(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, i
   for (size_t s = 0; s < lp.descs.size(); ++s) {
     const SeqDesc& sd = lp.descs[s];
     int64_t n_split, tps;
-    split_by_steps(sd, lp.shape, gqa, steps, min_tiles, n_split, tps);
+    split_by_steps(sd, lp.shape, steps, min_tiles, n_split, tps);
     if (n_split > 1) part += n_split * sd.chunk_len;
     // Workgroups of the fullest die: an even launch's equal runs (decode_slot) give it an
     // eighth, rounded up; decode_slot_dealt gives it one of every 8 whole (head, range) groups,
@@ -345,14 +346,14 @@ inline double launch_us(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, i
 // than its work spread evenly, and its work grows with its workgroups.  (Host time of one plan,
 // simulating every candidate -> now: 16 prompts of 1K median at 8/2 heads, d 64, 38 -> 13 us, and
 // their iteration, which plans twice, 85 -> 69 us; 8/1 heads, d 128, 15 -> 7 us.)
-inline int64_t choose_steps(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, int gqa, int num_cus,
+inline int64_t choose_steps(const LaunchPlan& lp, const LaunchWalks& lw, int h_kv, int num_cus,
                             const WalkCost& wc, int64_t base, int min_tiles, int64_t row_bytes,
                             int64_t max_rows, double& best_us) {
   const int64_t slots = (int64_t)num_cus * wc.wgs_per_cu;
   // (launches of very many rounds end within a walk or two of the even spread)
   best_us = lw.unsplit >= 8 * kMaxWaves * slots
                 ? even_us(lw, lw.longest, num_cus, wc)
-                : launch_us(lp, lw, h_kv, gqa, num_cus, wc, base, min_tiles, row_bytes);
+                : launch_us(lp, lw, h_kv, num_cus, wc, base, min_tiles, row_bytes);
   if (lw.unsplit >= kMaxWaves * slots || lw.longest <= min_tiles) return base;
   const int64_t allowed = std::min(max_rows, kMaxPartialBytes / row_bytes);
   int64_t best = base, prev = base;
@@ -365,15 +366,15 @@ inline int64_t choose_steps(const LaunchPlan& lp, const LaunchWalks& lw, int h_k
     prev = steps;
     if (even_us(lw, steps, num_cus, wc) + merge_us(part_rows, row_bytes) >= kWorth * best_us)
       return;
-    const double us = launch_us(lp, lw, h_kv, gqa, num_cus, wc, steps, min_tiles, row_bytes);
+    const double us = launch_us(lp, lw, h_kv, num_cus, wc, steps, min_tiles, row_bytes);
     if (us < kWorth * best_us) {
       best = steps;
       best_us = us;
     }
   };
-  const SplitSize uncut = split_size(lp, h_kv, gqa, lw.longest, min_tiles);
+  const SplitSize uncut = split_size(lp, h_kv, lw.longest, min_tiles);
   consider(lw.longest, uncut.part_rows);
-  const SplitSize finest = split_size(lp, h_kv, gqa, min_tiles, min_tiles);
+  const SplitSize finest = split_size(lp, h_kv, min_tiles, min_tiles);
   int64_t hi = lw.longest;  // the shortest ranges that fit the rounds so far, and their size
   SplitSize at_hi = uncut;
   for (int waves = 1; waves <= kMaxWaves; ++waves) {
@@ -390,7 +391,7 @@ inline int64_t choose_steps(const LaunchPlan& lp, const LaunchWalks& lw, int h_k
     }
     while (lo < hi) {
       probe = std::min(std::max(probe, lo), hi - 1);
-      const SplitSize size = split_size(lp, h_kv, gqa, probe, min_tiles);
+      const SplitSize size = split_size(lp, h_kv, probe, min_tiles);
       const bool fits = size.slots <= room;
       if (fits) {
         hi = probe;
@@ -414,7 +415,7 @@ inline void plan_launch(LaunchPlan& lp, int h_kv, int gqa, int64_t steps, int mi
   const ModeShape sh = lp.shape;
   for (SeqDesc& sd : lp.descs) {
     int64_t n_split, tps;
-    split_by_steps(sd, sh, gqa, steps, min_tiles, n_split, tps);
+    split_by_steps(sd, sh, steps, min_tiles, n_split, tps);
     sd.n_split = (int)n_split;
     sd.tiles_per_split = (int)tps;
     sd.dealt = sd.n_row_tiles > 1 && uneven_walks(sd, sh, gqa);
@@ -427,7 +428,7 @@ inline void plan_launch(LaunchPlan& lp, int h_kv, int gqa, int64_t steps, int mi
     for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
     auto walk = [&](int i) {
       const SeqDesc& sd = lp.descs[i];
-      return std::min<int64_t>(sd.tiles_per_split, sd.kv_len > 0 ? kv_tiles_of(sd, sh, gqa) : 0);
+      return std::min<int64_t>(sd.tiles_per_split, sd.kv_len > 0 ? kv_tiles_of(sd, sh) : 0);
     };
     std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return walk(a) > walk(b); });
     std::vector<SeqDesc> descs(order.size());
@@ -470,7 +471,7 @@ inline int64_t simple_steps(LaunchPlan& lp, int h_kv, int gqa, int target_wgs) {
   int64_t unsplit_wgs = 0, total_steps = 0, longest = 1;
   set_row_tiles(lp, gqa);
   for (const SeqDesc& sd : lp.descs) {
-    const int64_t kv_tiles = sd.kv_len > 0 ? kv_tiles_of(sd, lp.shape, gqa) : 0;
+    const int64_t kv_tiles = sd.kv_len > 0 ? kv_tiles_of(sd, lp.shape) : 0;
     unsplit_wgs += (int64_t)h_kv * sd.n_row_tiles;
     total_steps += (int64_t)h_kv * sd.n_row_tiles * kv_tiles;
     longest = std::max(longest, kv_tiles);
@@ -514,17 +515,17 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
   plan.keys.key_split = true;
   // Row-split mode: 4 wavefronts x (32 * q_blocks) rows, 64-key tiles.
   plan.rows.q_blocks = max_rows >= 256 ? 2 : 1;
-  plan.rows.shape = ModeShape{kWaves * 32 * plan.rows.q_blocks, 64, window};
+  plan.rows.shape = ModeShape{kWaves * 32 * plan.rows.q_blocks, 64, window, gqa};
   // Key-split mode: one 32-row block, 128-key tiles (32 per wavefront).
   plan.keys.q_blocks = 1;
-  plan.keys.shape = ModeShape{32, 32 * kWaves, window};
+  plan.keys.shape = ModeShape{32, 32 * kWaves, window, gqa};
   constexpr int kMinTiles = 4;
   const int64_t row_bytes = (int64_t)h_q * (head_dim + 1) * sizeof(float);
   int64_t keys_steps = 1, rows_steps = 1, keys_rows = 0, min_rows = 0;
   int keys_min_tiles = kMinTiles;
   if (!plan.rows.descs.empty()) {
     rows_steps = simple_steps(plan.rows, h_kv, gqa, num_cus);
-    min_rows = split_size(plan.rows, h_kv, gqa, rows_steps, kMinTiles).part_rows;
+    min_rows = split_size(plan.rows, h_kv, rows_steps, kMinTiles).part_rows;
   }
   // token rows of partials that fit the budget (the workspace's two arrays are rounded up to
   // 256 bytes each, which can cost the last rows)
@@ -532,7 +533,7 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
   while (fit > 0 && partial_bytes(fit, h_q, head_dim) > budget) --fit;
   if (!plan.keys.descs.empty()) {
     keys_steps = simple_steps(plan.keys, h_kv, gqa, num_cus * 8);
-    const SplitSize simple = split_size(plan.keys, h_kv, gqa, keys_steps, kMinTiles);
+    const SplitSize simple = split_size(plan.keys, h_kv, keys_steps, kMinTiles);
     const int64_t rows_min = min_rows;
     min_rows += simple.part_rows;
     // About 8 workgroups a compute unit are what a call has to bring scratch for.  Walks of 6 to 24
@@ -544,7 +545,7 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
     // heads, 87.2 -> 88.9); long walks fill their rounds with 8.
     const int64_t six = simple_steps(plan.keys, h_kv, gqa, num_cus * 6);
     if (six >= 6 && six <= kShortWalkTiles) keys_steps = six;
-    keys_rows = split_size(plan.keys, h_kv, gqa, keys_steps, kMinTiles).part_rows;
+    keys_rows = split_size(plan.keys, h_kv, keys_steps, kMinTiles).part_rows;
     // A launch that leaves compute units idle at ranges of 4 tiles, and is merged anyway, takes the
     // shortest ranges that find a unit each: a walk is a chain of trips to HBM, 1.2 us a tile.  (One
     // decode of 2048 at 32/8 heads 14.4 -> 13.6 us a pass, of 8000 19.8 -> 14.8, 8 of 2000 at 8/1
@@ -553,7 +554,7 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
     const int64_t launches = ceil_div((int64_t)plan.keys.descs.size(), kMaxInlineSeq);
     if (simple.part_rows > 0 && simple.items < num_cus * launches)
       for (int steps = 1; steps < kMinTiles; ++steps) {
-        const SplitSize fine = split_size(plan.keys, h_kv, gqa, steps, steps);
+        const SplitSize fine = split_size(plan.keys, h_kv, steps, steps);
         if (fine.items > num_cus * launches) continue;
         if (fine.part_rows + rows_min <= fit) {
           keys_steps = steps;
@@ -566,7 +567,7 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
   if (!plan.rows.descs.empty()) {
     if ((int)plan.rows.descs.size() <= kMaxPlannedSeqs) {
       double us, small_us;
-      rows_steps = choose_steps(plan.rows, launch_walks(plan.rows, h_kv, gqa), h_kv, gqa, num_cus,
+      rows_steps = choose_steps(plan.rows, launch_walks(plan.rows, h_kv, gqa), h_kv, num_cus,
                                 walk_cost(head_dim, plan.rows.q_blocks), rows_steps, kMinTiles,
                                 row_bytes, fit - keys_rows, us);
       // The small workgroups as an alternative, `least` to `most` of them, where the estimate falls
@@ -580,9 +581,9 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
         set_row_tiles(small, gqa);
         const LaunchWalks walks = launch_walks(small, h_kv, gqa);
         if (even_us(walks, walks.longest, num_cus, cost) >= worth * us) return;
-        const int64_t steps = choose_steps(small, walks, h_kv, gqa, num_cus, cost, INT32_MAX, kMinTiles,
+        const int64_t steps = choose_steps(small, walks, h_kv, num_cus, cost, INT32_MAX, kMinTiles,
                                            row_bytes, fit - keys_rows, small_us);
-        const int64_t slots = split_size(small, h_kv, gqa, steps, kMinTiles).slots;
+        const int64_t slots = split_size(small, h_kv, steps, kMinTiles).slots;
         if (steps <= short_tiles) worth = worth_short;
         if (small_us < worth * us && slots >= least && slots <= most) {
           plan.rows = std::move(small);
