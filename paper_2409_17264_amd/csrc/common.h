@@ -241,4 +241,12 @@ __device__ __forceinline__ float sum_halves(float x) {
   return __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
 }
 
+// Stores 4 elements.
+__device__ __forceinline__ void store4(float* to, const f32x4& v) {
+  *reinterpret_cast<f32x4*>(to) = v;
+}
+__device__ __forceinline__ void store4(__bf16* to, const f32x4& v) {
+  *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(v, bf16x4);
+}
+
 }  // namespace medha

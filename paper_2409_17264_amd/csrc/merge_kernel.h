@@ -61,13 +61,6 @@ __device__ __forceinline__ void fold_partials(const float* __restrict__ part_o,
   }
 }
 
-__device__ __forceinline__ void store4(float* to, const f32x4& v) {
-  *reinterpret_cast<f32x4*>(to) = v;
-}
-__device__ __forceinline__ void store4(__bf16* to, const f32x4& v) {
-  *reinterpret_cast<bf16x4*>(to) = __builtin_convertvector(v, bf16x4);
-}
-
 template <bool kNan = false, class Out>
 __device__ __forceinline__ void finish_merge(const MergeState& st, int d4,
                                              Out* __restrict__ out_row,

@@ -120,10 +120,26 @@ struct TileGeom {
 // clamped to the last one: they are masked, but must be finite.
 typedef const int32_t __attribute__((address_space(4))) * ConstI32Ptr;
 
-template <int D, int NW>
-__device__ __forceinline__ int tile_page(ConstI32Ptr pt, int tile, int kv_total, int wave) {
+// The keys of a walk over all of a sequence's: tile i of the walk is its tile i.
+struct AllKeys {
+  int kv_total;
+  __device__ __forceinline__ int tile(int i) const { return i; }
+  // whether every key of 64-key tile t is read
+  __device__ __forceinline__ bool whole(int t) const { return (t + 1) * 64 <= kv_total; }
+  // page of the keys from `row` on (16 or fewer, of one page); slot of one of them
+  __device__ __forceinline__ int page_index(int t, int row) const {
+    return min(t * 64 + row, kv_total - 1) >> 4;
+  }
+  __device__ __forceinline__ int slot(int t, int row) const {
+    return min(t * 64 + row, kv_total - 1) & 15;
+  }
+};
+
+template <int D, int NW, class Keys>
+__device__ __forceinline__ int tile_page(ConstI32Ptr pt, int tile, const Keys& keys, int wave) {
   using G = TileGeom<D, NW>;
-  const int idx = min(tile * G::kTileKeys + wave * G::kRowsPerWave, kv_total - 1) >> 4;
+  static_assert(G::kTileKeys == 64, "tiles of Keys");
+  const int idx = keys.page_index(tile, wave * G::kRowsPerWave);
   return pt[__builtin_amdgcn_readfirstlane(idx)];
 }
 
@@ -153,13 +169,13 @@ struct TileLoader {
 
   // Loads K and / or V rows row0.. of tile `tile`; page = id of the page holding them (see
   // tile_page()), k_stage / v_stage = LDS addresses of the tile's places in the ring.
-  template <bool K, bool V, bool kOnce>
-  __device__ __forceinline__ void issue(const AttnArgs& args, int page, int tile, int kv_total,
+  template <bool K, bool V, bool kOnce, class Args, class Keys>
+  __device__ __forceinline__ void issue(const Args& args, int page, int tile, const Keys& keys,
                                         int kv_head, uint32_t k_stage, uint32_t v_stage) const {
     const int64_t page_off = ((int64_t)page * args.h_kv + kv_head) * (kPageSize * D * 2);
     const char* kp = reinterpret_cast<const char*>(args.k_pool) + page_off;  // wave-uniform
     const char* vp = reinterpret_cast<const char*>(args.v_pool) + page_off;
-    if ((tile + 1) * G::kTileKeys <= kv_total) {
+    if (keys.whole(tile)) {
 #pragma unroll
       for (int j = 0; j < G::kInstrPerWave; ++j) {
         const uint32_t lds_off = (row0 + j * G::kRowsPerInstr) * (D * 2);  // wave-uniform
@@ -167,17 +183,17 @@ struct TileLoader {
         if (V) async_load16<kOnce>(vp, v_off[j], v_stage + lds_off);
       }
     } else {
-      // last, ragged tile: keys past the end are clamped to the last one (masked, but finite)
+      // a ragged tile: keys past the end are clamped to the last one (masked, but finite)
 #pragma unroll
       for (int j = 0; j < G::kInstrPerWave; ++j) {
         const int row = row0 + j * G::kRowsPerInstr + r_in;
-        const int t = min(tile * G::kTileKeys + row, kv_total - 1);
+        const int slot = keys.slot(tile, row);
         const uint32_t lds_off = (row0 + j * G::kRowsPerInstr) * (D * 2);
         if (K)
-          async_load16<kOnce>(kp, (uint32_t)((t & 15) * (D * 2) + Swz<D>::k(row, pos) * 16),
+          async_load16<kOnce>(kp, (uint32_t)(slot * (D * 2) + Swz<D>::k(row, pos) * 16),
                               k_stage + lds_off);
         if (V)
-          async_load16<kOnce>(vp, (uint32_t)((t & 15) * (D * 2) + Swz<D>::v(row, pos) * 16),
+          async_load16<kOnce>(vp, (uint32_t)(slot * (D * 2) + Swz<D>::v(row, pos) * 16),
                               v_stage + lds_off);
       }
     }
@@ -670,9 +686,11 @@ __device__ __forceinline__ void forget(T (&x)[N]) {
 // compile-time, so the change-over happens between rounds of 4 (6) tiles: up to 3 (5) fully
 // visible tiles take the masked form, which costs each about a fifth more; draining the ring
 // and filling it again at the exact tile (as two walks) costs 3 to 4 tiles' time.
-template <int D, int NW, int NV, bool kOnce>
-__device__ __forceinline__ void run_tiles(RowBlock<D>& rb, const AttnArgs& args, ConstI32Ptr pt,
-                                          int kt_a, int kt_mid, int kt_b, int kv_total,
+//
+// Tiles are counted along the walk; `keys` says which they are (AllKeys: those themselves).
+template <int D, int NW, int NV, bool kOnce, class Rows, class Args, class Keys>
+__device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Ptr pt,
+                                          int kt_a, int kt_mid, int kt_b, const Keys& keys,
                                           int kv_head, const Ring& ring,
                                           const TileLoader<D, NW>& ld, int wave, int lane) {
   using G = TileGeom<D, NW>;
@@ -691,7 +709,7 @@ __device__ __forceinline__ void run_tiles(RowBlock<D>& rb, const AttnArgs& args,
       page_2 = page_1;
       page_1 = page_next;
     }
-    page_next = tile_page<D, NW>(pt, min(tile, last), kv_total, wave);
+    page_next = tile_page<D, NW>(pt, keys.tile(min(tile, last)), keys, wave);
   };
   // Issues K tile `tile` into K stage k_stage and V tile `tile` - kLag into V stage v_stage, if that
   // is one (tiles past the walk's end: the last one again, harmlessly).  With the short ring V goes
@@ -700,12 +718,14 @@ __device__ __forceinline__ void run_tiles(RowBlock<D>& rb, const AttnArgs& args,
     const uint32_t k_lds = ring.lds_addr + decltype(k_stage)::value * kTile;
     const uint32_t v_lds = ring.lds_addr + (R::kK + decltype(v_stage)::value) * kTile;
     if constexpr (R::kLag == 0) {
-      ld.template issue<true, true, kOnce>(args, page_next, min(tile, last), kv_total, kv_head, k_lds, v_lds);
+      ld.template issue<true, true, kOnce>(args, page_next, keys.tile(min(tile, last)), keys, kv_head, k_lds,
+                                           v_lds);
     } else {
       if constexpr (decltype(v_stage)::value >= 0)
-        ld.template issue<false, true, kOnce>(args, page_2, min(tile - R::kLag, last), kv_total, kv_head, 0,
-                                       v_lds);
-      ld.template issue<true, false, kOnce>(args, page_next, min(tile, last), kv_total, kv_head, k_lds, 0);
+        ld.template issue<false, true, kOnce>(args, page_2, keys.tile(min(tile - R::kLag, last)), keys,
+                                              kv_head, 0, v_lds);
+      ld.template issue<true, false, kOnce>(args, page_next, keys.tile(min(tile, last)), keys, kv_head,
+                                            k_lds, 0);
     }
   };
   // loads of the iteration before that its successor's barrier leaves in flight
@@ -748,11 +768,11 @@ __device__ __forceinline__ void run_tiles(RowBlock<D>& rb, const AttnArgs& args,
         const char* k_next = ring.base + ((s + 1) % R::kK) * kTile;
         const char* v_cur = ring.base + (s % R::kV) * kTile;  // + the bias in rb.v_off
         if constexpr (s & 1)
-          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, cur * G::kTileKeys,
-                                                     half, issue_loads);
+          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, keys.tile(cur) * 64, half,
+                                                     issue_loads);
         else
-          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s0, s1, cur * G::kTileKeys,
-                                                     half, issue_loads);
+          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s0, s1, keys.tile(cur) * 64, half,
+                                                     issue_loads);
         // The scalar load of the next page id goes HERE, after the tile's last LDS read has
         // been consumed and before the barrier: scalar loads and LDS reads share one
         // counter and scalar loads return out of order, so with one in flight every wait for
@@ -786,15 +806,54 @@ __device__ __forceinline__ void run_tiles(RowBlock<D>& rb, const AttnArgs& args,
     constexpr bool kMask = decltype(mask)::value;
     const char* v_last = ring.base + ((last - kt_a) % R::kV) * kTile;  // + the bias in rb.v_off
     if ((last - kt_a) & 1)
-      rb.template fused<kMask, false, false>(nullptr, v_last, s1, s0, last * G::kTileKeys, half, [] {});
+      rb.template fused<kMask, false, false>(nullptr, v_last, s1, s0, keys.tile(last) * 64, half, [] {});
     else
-      rb.template fused<kMask, false, false>(nullptr, v_last, s0, s1, last * G::kTileKeys, half, [] {});
+      rb.template fused<kMask, false, false>(nullptr, v_last, s0, s1, keys.tile(last) * 64, half, [] {});
   };
   if (kt_u == kt_b)
     final_tile(std::false_type{});
   else
     final_tile(std::true_type{});
   ring_barrier<0>();
+}
+
+// O times `inv` goes out through LDS (the ring is done with: run_tiles() ends in a barrier), 32 rows per
+// wavefront in a place of its own.  In the registers a lane holds 4 elements here and there of
+// one row, which would leave as 32-byte pieces of 32 rows per instruction; turned in LDS, an
+// instruction writes whole rows.  The 16-byte column is XORed with the row, so neither
+// direction conflicts.  (The smallest prefill, 20 tiles: kernel 12.4 -> 11.8 us; 3584 tokens at
+// 8/2 heads 71 -> 67.5 us; eight prompts, 218 MB of O, 350 -> 347 us.)
+template <int D, int NW, int kLdsBytes, class Rows, class Out>
+__device__ __forceinline__ void write_rows(const Rows& rb, char* lds, float inv, Out* o_base,
+                                           int64_t row_base, int tok, int hq, int h_q, int wg_row0,
+                                           int n_rows, int wave, int lane) {
+  const int col = lane & 31, half = lane >> 5;
+  constexpr int kCols = D / 4, kRowsPerStore = 64 / kCols;
+  static_assert(NW * 32 * D * 4 <= kLdsBytes, "O of the workgroup fits the ring");
+  char* turn = lds + wave * (32 * D * 4);
+#pragma unroll
+  for (int db = 0; db < Rows::kDBlocks; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 v;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = rb.o[db][4 * i + j] * inv;
+      const int c = db * 8 + 2 * i + half;
+      *reinterpret_cast<f32x4*>(turn + col * (D * 4) + ((c ^ col) & (kCols - 1)) * 16) = v;
+    }
+  asm volatile("" ::: "memory");  // (one wavefront's LDS accesses stay in order)
+  const int row0 = wg_row0 + wave * 32;  // the wavefront's rows that exist start here
+  const int tok0 = __builtin_amdgcn_readfirstlane(tok);
+  Out* const o_out = o_base + (row_base + tok0) * h_q * D;
+  const int rel = (tok - tok0) * h_q + hq;  // row of the output counted from o_out
+#pragma unroll
+  for (int k = 0; k < 32 / kRowsPerStore; ++k) {
+    const int row = k * kRowsPerStore + lane / kCols, c = lane % kCols;
+    const int to = __shfl(rel, row);
+    const f32x4 v =
+        *reinterpret_cast<const f32x4*>(turn + row * (D * 4) + ((c ^ row) & (kCols - 1)) * 16);
+    if (row0 + row < n_rows) store4(o_out + (int64_t)to * D + c * 4, v);
+  }
 }
 
 // (the launch bound is 512 also for the 4-wavefront variant: it makes the compiler budget
@@ -858,8 +917,8 @@ __global__ void __launch_bounds__(512) prefill_kernel(const AttnArgs args) {
   ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
   TileLoader<D, NW> loader;
   loader.init(wave, lane);
-  run_tiles<D, NW, NV, kOnce>(rb, args, pt, kt_begin, kt_mid, kt_end, kv_total, kv_head, stages, loader,
-                       wave, lane);
+  run_tiles<D, NW, NV, kOnce>(rb, args, pt, kt_begin, kt_mid, kt_end, AllKeys{kv_total}, kv_head, stages,
+                              loader, wave, lane);
 
   const bool direct = sd.n_split == 1;
   float* o_base = direct ? args.out : args.part_o;
@@ -871,38 +930,8 @@ __global__ void __launch_bounds__(512) prefill_kernel(const AttnArgs args) {
   const float lse = lt > 0.f ? (rb.m + fast_log2(lt)) * kLn2 : -INFINITY;
   if (valid && half == 0) l_base[(row_base + tok) * args.h_q + hq] = lse;
 
-  // O goes out through LDS (the ring is done with: run_tiles() ends in a barrier), 32 rows per
-  // wavefront in a place of its own.  In the registers a lane holds 4 elements here and there of
-  // one row, which would leave as 32-byte pieces of 32 rows per instruction; turned in LDS, an
-  // instruction writes whole rows.  The 16-byte column is XORed with the row, so neither
-  // direction conflicts.  (The smallest prefill, 20 tiles: kernel 12.4 -> 11.8 us; 3584 tokens at
-  // 8/2 heads 71 -> 67.5 us; eight prompts, 218 MB of O, 350 -> 347 us.)
-  constexpr int kCols = D / 4, kRowsPerStore = 64 / kCols;
-  static_assert(NW * 32 * D * 4 <= Shape::kLdsBytes, "O of the workgroup fits the ring");
-  char* turn = lds + wave * (32 * D * 4);
-#pragma unroll
-  for (int db = 0; db < RowBlock<D>::kDBlocks; ++db)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      f32x4 v;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = rb.o[db][4 * i + j] * inv;
-      const int c = db * 8 + 2 * i + half;
-      *reinterpret_cast<f32x4*>(turn + col * (D * 4) + ((c ^ col) & (kCols - 1)) * 16) = v;
-    }
-  asm volatile("" ::: "memory");  // (one wavefront's LDS accesses stay in order)
-  const int row0 = wg_row0 + wave * 32;  // the wavefront's rows that exist start here
-  const int tok0 = __builtin_amdgcn_readfirstlane(tok);
-  float* const o_out = o_base + (row_base + tok0) * args.h_q * D;
-  const int rel = (tok - tok0) * args.h_q + hq;  // row of the output counted from o_out
-#pragma unroll
-  for (int k = 0; k < 32 / kRowsPerStore; ++k) {
-    const int row = k * kRowsPerStore + lane / kCols, c = lane % kCols;
-    const int to = __shfl(rel, row);
-    const f32x4 v =
-        *reinterpret_cast<const f32x4*>(turn + row * (D * 4) + ((c ^ row) & (kCols - 1)) * 16);
-    if (row0 + row < n_rows) *reinterpret_cast<f32x4*>(o_out + (int64_t)to * D + c * 4) = v;
-  }
+  write_rows<D, NW, Shape::kLdsBytes>(rb, lds, inv, o_base, row_base, tok, hq, args.h_q, wg_row0, n_rows,
+                                      wave, lane);
 }
 
 }  // namespace medha

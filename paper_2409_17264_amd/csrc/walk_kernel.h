@@ -420,4 +420,85 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
   }
 }
 
+// ---------------------------------------------------------------- row-split, bf16 cache
+
+// The 64-key tiles of a walk, for run_tiles().
+struct WalkKeys {
+  KeyWalk w;
+  __device__ __forceinline__ int tile(int i) const { return w.tile(i); }
+  __device__ __forceinline__ bool whole(int t) const {
+    return (t * 64 >= w.lo && (t + 1) * 64 <= w.end) || (t + 1) * 64 <= w.first;
+  }
+  __device__ __forceinline__ int page_index(int t, int row) const {
+    return PageRead(w, t * 64 + (row & ~(kPageSize - 1))).page_index;
+  }
+  __device__ __forceinline__ int slot(int t, int row) const {
+    return PageRead(w, t * 64 + (row & ~(kPageSize - 1))).slot(row & (kPageSize - 1));
+  }
+};
+
+// Chunks: a workgroup of NW wavefronts owns NW * 32 query rows of one KV head and walks 64-key tiles,
+// as prefill_kernel does, along the tiles of its rows' windows.
+template <int D, int NW, int NV>
+__global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
+  using Shape = PrefillShape<D, NW, NV>;
+  using Rows = RowBlock<D, WindowMask>;
+  __shared__ __attribute__((aligned(1024))) char lds[Shape::kLdsBytes];
+  const Ring stages{lds, lds_address(lds)};
+
+  const SeqDesc* descs = args.inline_descs;
+  const int seq = find_seq_slot(descs, args.n_seq, blockIdx.x);
+  const SeqDesc sd = uniform(descs[seq]);
+  const SlotItem it =
+      row_split_item(sd, blockIdx.x - sd.work_start, args.h_kv, seq == args.n_seq - 1);
+  if (!it.valid) return;
+  const int kv_head = it.kv_head, split = it.split;
+
+  const int gqa = args.h_q / args.h_kv;
+  const int n_rows = sd.chunk_len * gqa;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int col = lane & 31, half = lane >> 5;
+
+  Rows rb;
+  rb.init(fabsf(args.scale_log2), lane, Shape::kVBias);
+  const int wg_row0 = it.row_tile * Shape::kRowsPerWg;
+  const int r = wg_row0 + wave * 32 + col;
+  const bool valid = r < n_rows;
+  const int rr = valid ? r : (n_rows - 1);
+  const int tok = rr / gqa;
+  const int hq = kv_head * gqa + rr % gqa;
+  rb.mask.set(sd.prefix_len + tok, args.window);
+  Bf16Block<D>::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
+
+  const int last_row = min(n_rows, wg_row0 + Shape::kRowsPerWg) - 1;
+  const WalkKeys keys{make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,
+                                args.window, 64)};
+  const int kt_begin = split * sd.tiles_per_split;
+  const int kt_end = min(keys.w.n, kt_begin + sd.tiles_per_split);
+  const int kt_mid = max(kt_begin, min(kt_end, keys.w.n_full));
+  ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
+  TileLoader<D, NW> loader;
+  loader.init(wave, lane);
+  run_tiles<D, NW, NV, false>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, stages, loader, wave,
+                              lane);
+
+  const bool direct = sd.n_split == 1;
+  void* o_base = direct ? args.out : args.part_o;
+  float* l_base = direct ? args.lse : args.part_lse;
+  const int64_t row_base =
+      direct ? (int64_t)sd.out_row : (int64_t)sd.part_row + (int64_t)split * sd.chunk_len;
+  // (a range without a tile has the sum 0; a NaN among a row's keys reaches its result)
+  const float lt = rb.row_sum();
+  const float inv = lt != 0.f ? 1.f / lt : 0.f;
+  const float lse = lt != 0.f ? (rb.m + fast_log2(lt)) * kLn2 : -INFINITY;
+  if (valid && half == 0) l_base[(row_base + tok) * args.h_q + hq] = lse;
+  if (direct && args.out_bf16)
+    write_rows<D, NW, Shape::kLdsBytes>(rb, lds, inv, static_cast<__bf16*>(o_base), row_base, tok, hq,
+                                        args.h_q, wg_row0, n_rows, wave, lane);
+  else
+    write_rows<D, NW, Shape::kLdsBytes>(rb, lds, inv, static_cast<float*>(o_base), row_base, tok, hq,
+                                        args.h_q, wg_row0, n_rows, wave, lane);
+}
+
 }  // namespace medha

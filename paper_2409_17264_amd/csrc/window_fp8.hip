@@ -96,6 +96,17 @@ hipError_t launch_keys(const WalkArgs& a, int grid, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_rows(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStream_t stream) {
+  if (lp.q_blocks == 2)
+    hipLaunchKernelGGL((row_walk_kernel<D, 8, 4>), dim3(grid), dim3(512), 0, stream, a);
+  else if (lp.paired)
+    hipLaunchKernelGGL((row_walk_kernel<128, 4, 2>), dim3(grid), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((row_walk_kernel<D, 4, 4>), dim3(grid), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
 template <int D, class Out>
 hipError_t launch_merge(const MergeArgs& m, int max_split, hipStream_t stream) {
   if (max_split > kWideMergeSplits) {
@@ -130,7 +141,9 @@ hipError_t launch_walks(const LaunchPlan& lp, WalkArgs& a, hipStream_t stream) {
       sd.row_rank -= rank0;
       max_split = std::max(max_split, sd.n_split);
     }
-    hipError_t e = launch_keys<D>(a, slot1 - slot0, stream);
+    if (slot1 == slot0) continue;
+    hipError_t e = lp.key_split ? launch_keys<D>(a, slot1 - slot0, stream)
+                                : launch_rows<D>(lp, a, slot1 - slot0, stream);
     if (e != hipSuccess) return e;
     if (max_split == 1) continue;
     MergeArgs m{};
@@ -158,9 +171,9 @@ bool window_of(int32_t keys, int32_t sinks, bool optional, Window& w) {
 }
 
 Plan walk_plan(const std::vector<SeqInput>& seqs, int h_q, int h_kv, int d, size_t budget,
-               const Window& w) {
+               const Window& w, bool fp8) {
   return make_plan(seqs.data(), (int)seqs.size(), h_q, h_kv, d, current_num_cus(), budget, w,
-                   INT64_MAX);
+                   fp8 ? INT64_MAX : 32);
 }
 
 size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32_t batch,
@@ -179,7 +192,8 @@ size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32
     row += chunk_len[b];
     if (row > INT32_MAX) return 0;
   }
-  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w).workspace_bytes();
+  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w, optional)
+      .workspace_bytes();
 }
 
 // A call on either cache.  `kv` describes its pools, `scale` is null for the bf16 one; `alloc`: asked
@@ -217,7 +231,8 @@ int walk_attn(const void* q, const medha_kv_cache* kv, const void* scale, const 
     if (row > INT32_MAX) return MEDHA_ERR_INVALID_ARG;
   }
   const Plan plan = walk_plan(seqs, num_q_heads, kv->num_kv_heads, kv->head_dim,
-                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window);
+                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window,
+                              scale != nullptr);
   if (alloc) {
     workspace_bytes = plan.workspace_bytes();
     workspace = alloc(workspace_bytes, context);
@@ -246,7 +261,9 @@ int walk_attn(const void* q, const medha_kv_cache* kv, const void* scale, const 
   a.out_bf16 = out_type == MEDHA_OUT_BF16;
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const auto launch = kv->head_dim == 128 ? launch_walks<128> : launch_walks<64>;
-  return launch(plan.keys, a, stream) == hipSuccess ? MEDHA_OK : MEDHA_ERR_HIP;
+  if (launch(plan.rows, a, stream) != hipSuccess || launch(plan.keys, a, stream) != hipSuccess)
+    return MEDHA_ERR_HIP;
+  return MEDHA_OK;
 }
 
 int attn_bf16(const void* q, const medha_kv_cache* kv, const int32_t* page_table,

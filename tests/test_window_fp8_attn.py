@@ -115,3 +115,24 @@ def test_windows(heads, fp8, prefix, chunk, window, sinks):
 def test_the_8_bit_cache_without_a_window(heads, prefix, chunk):
     c = Case(*heads, prefix, chunk, None, 0, True, seed=len(prefix) + chunk[0])
     c.check(*c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(8, 1, 128), (4, 2, 64)])
+@pytest.mark.parametrize("fp8, prefix, chunk, window, sinks", [
+    (False, [9000], [130], 4999, 33), (False, [9000], [64], 7000, 0), (False, [0], [1500], 1100, 70),
+    (False, [5000, 70], [1, 700], 2500, 4), (True, [9000], [130], 4999, 33), (True, [9000], [64], None, 0),
+    (True, [0], [1500], None, 0), (True, [0], [1500], 1100, 70), (True, [5000, 70], [1, 700], None, 0)])
+def test_long_walks(heads, fp8, prefix, chunk, window, sinks):
+    c = Case(*heads, prefix, chunk, window, sinks, fp8, seed=sum(chunk))
+    c.check(*c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k_std", [6.0, 0.0])
+@pytest.mark.parametrize("fp8, window", [(False, 3000), (True, 3000), (True, None)])
+def test_peaked_and_flat_rows(fp8, window, k_std):
+    """Keys six times as long (one key carries its row, at places that shift from row to row), and keys
+    that are all zero."""
+    c = Case(4, 1, 128, [4000], [100], window, 5, fp8, seed=4, k_std=k_std)
+    c.check(*c.run())
