@@ -484,14 +484,12 @@ inline int64_t simple_steps(LaunchPlan& lp, int h_kv, int gqa, int target_wgs) {
 // if its partials fit it (so that every workspace of the reported size gives the same plan, whatever
 // the choices on the way to it look at), and otherwise takes the KV ranges that are expected to be
 // fastest among those whose partials do; the simple rule's need (`min_bytes`) is the least a call has
-// to bring.  `window`: of the rows; `most_keys_rows`: sequences of more (token, head-in-group) rows are
-// split by rows.
+// to bring.  `window`: of the rows.
 inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int head_dim,
-                      int num_cus, size_t budget = SIZE_MAX, const Window& window = {},
-                      int64_t most_keys_rows = 32) {
+                      int num_cus, size_t budget = SIZE_MAX, const Window& window = {}) {
   Plan plan;
   if (budget != SIZE_MAX) {
-    plan = make_plan(seqs, batch, h_q, h_kv, head_dim, num_cus, SIZE_MAX, window, most_keys_rows);
+    plan = make_plan(seqs, batch, h_q, h_kv, head_dim, num_cus, SIZE_MAX, window);
     if (plan.part_rows == 0 || plan.bytes <= budget) return plan;
     plan = Plan{};
   }
@@ -506,10 +504,10 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
     sd.prefix_len = seqs[b].prefix_len;
     sd.kv_len = seqs[b].kv_len >= 0 ? seqs[b].kv_len : sd.prefix_len + sd.chunk_len;
     const int64_t n_rows = (int64_t)sd.chunk_len * gqa;
-    LaunchPlan& lp = n_rows <= most_keys_rows ? plan.keys : plan.rows;
+    LaunchPlan& lp = n_rows <= 32 ? plan.keys : plan.rows;
     lp.descs.push_back(sd);
     lp.seq_index.push_back(b);
-    if (n_rows > most_keys_rows) max_rows = std::max(max_rows, (int)std::min<int64_t>(n_rows, 1 << 30));
+    if (n_rows > 32) max_rows = std::max(max_rows, (int)std::min<int64_t>(n_rows, 1 << 30));
   }
   plan.rows.num_cus = plan.keys.num_cus = num_cus;
   plan.keys.key_split = true;

@@ -402,8 +402,23 @@ struct RowBlock {
     softmax_pv<NKB, MASK>(s, v_lds, vop, key0, half);
   }
 
+  // The K side of a tile in fused(): slot i's operand, read three slots ahead, and its product.
+  struct KSide {
+    const RowBlock& rb;
+    const char* k_lds;
+    bf16x8 ka[4];
+    __device__ __forceinline__ KSide(const RowBlock& rows, const char* k) : rb(rows), k_lds(k) {}
+    __device__ __forceinline__ void read(int i) {
+      ka[i & 3] = *reinterpret_cast<const bf16x8*>(k_lds + (i & 1) * 32 * (D * 2) + rb.k_off[i >> 1]);
+    }
+    template <int i>
+    __device__ __forceinline__ void multiply(f32x16 (&s)[2]) {
+      s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i & 3], rb.q[i >> 1], s[i & 1], 0, 0, 0);
+    }
+  };
+
   // Steady state of the 64-key tile walk: softmax_pv() of the current tile (scores
-  // sc, V tile v_cur, first key key0) and qk() of the next tile (K tile k_next, scores
+  // sc, V tile v_cur, first key key0) and qk() of the next tile (K side `next`, scores
   // into sn) as ONE stream of kSlots slots.  Slot i holds one MFMA -- first the
   // next tile's S^T = K Q^T, then the current tile's O^T += V^T P^T, slice by slice --
   // the LDS read of the operand of slot i+3, and a share of the current tile's softmax
@@ -472,13 +487,14 @@ struct RowBlock {
 
   //
   // QK false leaves the next tile out (the walk's last tile): the same slots without
-  // their K reads and S^T MFMAs; k_next and sn are not touched.  SPEC false takes the
+  // their K reads and S^T MFMAs; `next` and sn are not touched.  SPEC false takes the
   // exact route (row maximum first) also on an unmasked tile: for the first tiles of a
   // walk, whose speculation would fail anyway, it is the cheaper of the two.
-  template <bool MASK, bool QK = true, bool SPEC = true, class Loads>
-  __device__ __forceinline__ void fused(const char* k_next, const char* v_cur, f32x16 (&sc)[2],
+  // `at_slot` is called at the end of every slot with its index: the loads of a tile further on.
+  template <bool MASK, bool QK = true, bool SPEC = true, class KSide, class AtSlot>
+  __device__ __forceinline__ void fused(KSide next, const char* v_cur, f32x16 (&sc)[2],
                                         f32x16 (&sn)[2], int key0, int half,
-                                        Loads issue_loads) {
+                                        AtSlot at_slot) {
     constexpr bool kSpec = SPEC && !MASK;
     constexpr int kQk = 2 * kSlices;       // MFMAs of the next tile's S^T
     constexpr int kPv = 4 * kDBlocks;      // MFMAs of the current tile's O^T
@@ -492,15 +508,14 @@ struct RowBlock {
     // failed check does not touch when it moves the reference point and rescales O.
     static_assert(2 * kSpan <= kQk && 4 * kSpan == kQk + 2 * kDBlocks, "checked before consumed");
     constexpr int kCheck0 = 2 * kSpan - 1 - kLead, kCheck1 = 4 * kSpan - 1;
-    bf16x8 ka[4], va[4];
+    bf16x8 va[4];
     uint32_t pw[4][4];  // P^T operands of the 4 slices as packed bf16 pairs
     float mx = -INFINITY, m_use = m, ls = 0.f;
     float pe_prev = 0.f;
 
     auto read_operand = [&](int i) {
       if (i < kQk) {
-        if (QK)
-          ka[i & 3] = *reinterpret_cast<const bf16x8*>(k_next + (i & 1) * 32 * (D * 2) + k_off[i >> 1]);
+        if (QK) next.read(i);
       } else if (i < kSlots) {
         const int j = i - kQk, g = j / kDBlocks, db = j % kDBlocks;
         const char* vp = v_cur + g * 16 * (D * 2) + v_off[db];
@@ -566,15 +581,14 @@ struct RowBlock {
       if constexpr (i % (kSlots / 4) == 0) __builtin_amdgcn_s_setprio(3 - i / (kSlots / 4));
       read_operand(i + 3);
       if constexpr (i < kQk) {
-        if constexpr (QK)
-          sn[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[i & 3], q[i >> 1], sn[i & 1], 0, 0, 0);
+        if constexpr (QK) next.template multiply<i>(sn);
       } else {
         constexpr int j = i - kQk, g = j / kDBlocks, db = j % kDBlocks;
         const uint4 w = make_uint4(pw[g][0], pw[g][1], pw[g][2], pw[g][3]);
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[i & 3], __builtin_bit_cast(bf16x8, w),
                                                         o[db], 0, 0, 0);
       }
-      if constexpr (i == kLoadSlot) issue_loads();
+      at_slot(slot_index);
       if constexpr (i + kLead < kSlots) share(std::integral_constant<int, i + kLead>{});
       if constexpr (kSpec && (i == kCheck0 || i == kCheck1)) {
         // ls covers the two slices just finished
@@ -760,12 +774,13 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
         // this wavefront's loads for the iteration have landed (the youngest may fly); after the
         // barrier everyone's have, and everyone is done with the stages refilled next
         ring_barrier<kYoungest>();
-        auto issue_loads = [&] {
+        auto issue_loads = [&](auto slot) {
+          if constexpr (decltype(slot)::value != Rows::kLoadSlot) return;
           asm volatile("" : "+s"(page_next));  // the page id is first needed here, not before
           issue(cur + 3, std::integral_constant<int, (s + 3) % R::kK>{},
                 std::integral_constant<int, (s + 3 - R::kLag) % R::kV>{});
         };
-        const char* k_next = ring.base + ((s + 1) % R::kK) * kTile;
+        const typename Rows::KSide k_next(rb, ring.base + ((s + 1) % R::kK) * kTile);
         const char* v_cur = ring.base + (s % R::kV) * kTile;  // + the bias in rb.v_off
         if constexpr (s & 1)
           rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, keys.tile(cur) * 64, half,
@@ -806,9 +821,9 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
     constexpr bool kMask = decltype(mask)::value;
     const char* v_last = ring.base + ((last - kt_a) % R::kV) * kTile;  // + the bias in rb.v_off
     if ((last - kt_a) & 1)
-      rb.template fused<kMask, false, false>(nullptr, v_last, s1, s0, keys.tile(last) * 64, half, [] {});
+      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s1, s0, keys.tile(last) * 64, half, [](auto) {});
     else
-      rb.template fused<kMask, false, false>(nullptr, v_last, s0, s1, keys.tile(last) * 64, half, [] {});
+      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s0, s1, keys.tile(last) * 64, half, [](auto) {});
   };
   if (kt_u == kt_b)
     final_tile(std::false_type{});

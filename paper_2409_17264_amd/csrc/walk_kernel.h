@@ -185,8 +185,8 @@ struct Rows8 : RowBlock<D, WindowMask> {
       }
   }
 
-  // k_lds: rows of D bytes, swizzled; scales: as the pool has them, [page][2][16].
-  template <int NKB>
+  // k_lds: rows of D bytes, swizzled; scales: a page's 32 bytes at every kStride.
+  template <int NKB, int kStride = kScaleBytesPerPage>
   __device__ __forceinline__ void qk(const char* k_lds, const char* scales, int lane,
                                      f32x16 (&s)[NKB]) const {
     const int col = lane & 31, half = lane >> 5;
@@ -195,7 +195,7 @@ struct Rows8 : RowBlock<D, WindowMask> {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
       const int row = kb * 32 + col;
-      const int ks = (uint8_t)scales[(row >> 4) * kScaleBytesPerPage + (row & 15)];
+      const int ks = (uint8_t)scales[(row >> 4) * kStride + (row & 15)];
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
         const int c = part * 4 + half * 2;
@@ -437,14 +437,322 @@ struct WalkKeys {
   }
 };
 
+// ---------------------------------------------------------------- row-split, 8-bit cache
+
+__device__ __forceinline__ void async_load4(const void* base_uniform, uint32_t lane_off,
+                                            uint32_t lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(lds_addr_uniform), "v"(lane_off), "s"(base_uniform)
+               : "m0", "memory");
+}
+
+// As ring_barrier(), and this wavefront's LDS writes are done.
+template <int N>
+__device__ __forceinline__ void ring_barrier_written() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// The workgroup's LDS: 4 stages each of K and V tiles as they come, D bytes a row, their scale bytes,
+// and two V tiles in bf16.
+template <int D, int NW>
+struct Fp8Ring {
+  static constexpr int kStages = 4;
+  static constexpr int kTile = 64 * D;  // K (or V) tile
+  static constexpr int kScales = NW * 256;  // a wavefront's 64 lanes' worth
+  static constexpr int kV = kStages * kTile, kS = 2 * kV, kV16 = kS + kStages * kScales;
+  static constexpr int kBytes = kV16 + 2 * (2 * kTile);
+  static constexpr int kLdsBytes = kBytes > NW * 32 * D * 4 ? kBytes : NW * 32 * D * 4;  // (write_rows)
+  // a tile's load instructions, 1 KiB each: every wavefront takes as many of K as of V, or, where
+  // there are fewer of each than wavefronts, the first half of the wavefronts K and the others V
+  static constexpr int kInstr = kTile / 1024, kRowsPerInstr = 1024 / D;
+  static constexpr bool kBoth = kInstr >= NW;
+  static constexpr int kPerWave = kBoth ? kInstr / NW : 1;
+  static constexpr int kLoads = (kBoth ? 2 * kPerWave : 1) + 1;
+  // the scale bytes of page p of a tile are where its first wavefront put them
+  static constexpr int kScaleStride = kBoth ? NW / 4 * 256 : 256;
+  // V rows a wavefront turns into bf16, and its lanes' bytes of them
+  static constexpr int kRowsPerWave = 64 / NW, kLaneBytes = kRowsPerWave * D / 64;
+};
+
+// Rows of one wavefront with what the tile walk needs of them.
+template <int D, int NW>
+struct TileRows8 : Rows8<D> {
+  using Base = Rows8<D>;
+  using R = Fp8Ring<D, NW>;
+  int k8_off[2 * Base::kParts];  // this lane's 16-byte pieces of key row `col`, within a K tile
+  int ks_off;                    // its scale byte within a stage's
+  int wave_page, k_pos, lane;
+
+  __device__ __forceinline__ void init(float scale, int ln, int wave) {
+    Base::init(scale, ln, R::kV16);
+    lane = ln;
+    const int col = ln & 31, half = ln >> 5;
+#pragma unroll
+    for (int i = 0; i < 2 * Base::kParts; ++i)
+      k8_off[i] = col * D + swz8<D>(col, (i >> 1) * 4 + half * 2 + (i & 1)) * 16;
+    ks_off = (col >> 4) * R::kScaleStride + (col & 15);
+  }
+
+  // Products n = 0, 1, ...: key block n & 1, head-dim part n >> 1, first with the high parts of Q and
+  // then with the low ones.  Each takes the time of two bf16 products: 2 slots of 4.
+  struct KSide {
+    const TileRows8& rb;
+    const char* k_lds;
+    const char* scales;
+    int ks[2];
+    i32x8 a[2];
+    __device__ __forceinline__ KSide(const TileRows8& rows, const char* k, const char* s)
+        : rb(rows), k_lds(k), scales(s) {}
+    __device__ __forceinline__ void load(int n) {
+      const char* at = k_lds + (n & 1) * 32 * D;
+      const i32x4 x = *reinterpret_cast<const i32x4*>(at + rb.k8_off[2 * (n >> 1)]);
+      const i32x4 y = *reinterpret_cast<const i32x4*>(at + rb.k8_off[2 * (n >> 1) + 1]);
+      a[n & 1] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    __device__ __forceinline__ void read(int i) {
+      if (i == 0) {
+        ks[0] = (uint8_t)scales[rb.ks_off];
+        ks[1] = (uint8_t)scales[rb.ks_off + 2 * R::kScaleStride];
+        load(0);
+      } else if (i % 4 == 3 && i / 4 + 1 < 2 * Base::kParts) {
+        load(i / 4 + 1);
+      }
+    }
+    template <int i>
+    __device__ __forceinline__ void multiply(f32x16 (&s)[2]) {
+      if constexpr (i % 2 == 0) {
+        constexpr int n = i / 4, kb = n & 1, part = n >> 1;
+        const i32x8& q = i % 4 == 0 ? rb.hi[part] : rb.lo[part];
+        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            a[kb], q, s[kb], 0, 0, 0, ks[kb], 0, i % 4 == 0 ? rb.hi_scale : rb.lo_scale);
+      }
+    }
+  };
+};
+
+// This wavefront's share of a tile's loads.
+template <int D, int NW>
+struct Fp8Loader {
+  using R = Fp8Ring<D, NW>;
+  uint32_t k_off[R::kPerWave], v_off[R::kPerWave];  // within the (page, KV head) block
+  int row0, r_in, pos;
+  bool values;  // !kBoth: this wavefront loads V
+
+  __device__ __forceinline__ void init(int wave, int lane) {
+    row0 = R::kBoth ? wave * R::kRowsPerWave : (wave & 3) * kPageSize;
+    values = !R::kBoth && wave >= 4;
+    r_in = lane / (D / 16);
+    pos = lane % (D / 16);
+#pragma unroll
+    for (int j = 0; j < R::kPerWave; ++j) {
+      const int row = row0 + j * R::kRowsPerInstr + r_in;
+      k_off[j] = (row & 15) * D + swz8<D>(row, pos) * 16;
+      v_off[j] = (row & 15) * D + pos * 16;
+    }
+  }
+  // `stage`: of the ring, with the wavefront's place among the scale bytes.
+  template <class Keys>
+  __device__ __forceinline__ void issue(const WalkArgs& args, int page, int tile, const Keys& keys,
+                                        int kv_head, uint32_t ring, int stage, int wave, int lane) const {
+    const int64_t block = (int64_t)page * args.h_kv + kv_head;
+    const char* kp = args.k_pool + block * (kPageSize * D);
+    const char* vp = args.v_pool + block * (kPageSize * D);
+    const uint32_t to = ring + stage * R::kTile;
+    auto load = [&](uint32_t ko, uint32_t vo, int j) {
+      const uint32_t at = to + (row0 + j * R::kRowsPerInstr) * D;
+      if constexpr (R::kBoth) {
+        async_load16<false>(kp, ko, at);
+        async_load16<false>(vp, vo, at + R::kV);
+      } else {
+        async_load16<false>(values ? vp : kp, values ? vo : ko, values ? at + R::kV : at);
+      }
+    };
+    if (keys.whole(tile)) {
+#pragma unroll
+      for (int j = 0; j < R::kPerWave; ++j) load(k_off[j], v_off[j], j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < R::kPerWave; ++j) {
+        const int row = row0 + j * R::kRowsPerInstr + r_in;
+        const int slot = keys.slot(tile, row);
+        load(slot * D + swz8<D>(row, pos) * 16, slot * D + pos * 16, j);
+      }
+    }
+    async_load4(args.scale + block * kScaleBytesPerPage, (lane & 7) * 4,
+                ring + R::kS + stage * R::kScales + wave * 256);
+  }
+};
+
+// The wavefront's V rows of a tile, from 8 bits to bf16 where the transposing reads expect them.
+template <int D, int NW>
+struct Fp8Convert {
+  using R = Fp8Ring<D, NW>;
+  static constexpr int kWords = R::kLaneBytes / 4;
+  static constexpr int kPieces = kWords > 4 ? kWords / 4 : 1;  // of 16 bytes (or one of 8)
+  static constexpr int kPieceRows = kWords > 4 ? R::kRowsPerWave / kPieces : R::kRowsPerWave;
+  static constexpr int kPieceWords = kWords / kPieces;
+  int in_off, out_off, row;
+  uint32_t raw[kWords];
+  float scale[kPieces];
+  uint2 half;
+
+  __device__ __forceinline__ void init(int wave, int lane) {
+    constexpr int kLanesPerRow = D / (4 * kPieceWords);
+    row = wave * R::kRowsPerWave + lane / kLanesPerRow;
+    const int at = lane % kLanesPerRow * kPieceWords;  // word of the row: 4 elements
+    in_off = R::kV + row * D + at * 4;
+    out_off = R::kV16 + row * (D * 2) + Swz<D>::v(row, at / 2) * 16;
+  }
+  template <class Keys>
+  __device__ __forceinline__ void read(const char* lds, int stage, int tile, const Keys& keys) {
+    const char* in = lds + stage * R::kTile + in_off;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const int r = row + p * kPieceRows;
+      const char* s = lds + R::kS + stage * R::kScales + (r >> 4) * R::kScaleStride + kPageSize;
+      scale[p] = __builtin_bit_cast(float, (uint32_t)(uint8_t)s[keys.slot(tile, r)] << 23);
+      if constexpr (kPieceWords == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(in + p * kPieceRows * D);
+        raw[4 * p] = x.x; raw[4 * p + 1] = x.y; raw[4 * p + 2] = x.z; raw[4 * p + 3] = x.w;
+      } else {
+        const uint2 x = *reinterpret_cast<const uint2*>(in);
+        raw[0] = x.x; raw[1] = x.y;
+      }
+    }
+  }
+  // word w of the lane's, written out behind every second one
+  template <int w>
+  __device__ __forceinline__ void convert(char* lds, int v16_stage) {
+    const uint2 x = dequantise4(raw[w], scale[w / kPieceWords]);
+    if constexpr (w % 2 == 0) {
+      half = x;
+    } else {
+      constexpr int p = w / kPieceWords, c = w % kPieceWords / 2;
+      *reinterpret_cast<uint4*>(lds + v16_stage * (2 * R::kTile) + out_off + p * kPieceRows * (D * 2) +
+                                c * 16) = make_uint4(half.x, half.y, x.x, x.y);
+    }
+  }
+};
+
+// Walks tiles [kt_a, kt_b) of a walk, those below kt_mid without a mask: run_tiles() over the 8-bit
+// cache.  At the barrier that opens iteration cur, K tile cur+1 and V tile cur+1 have landed as they
+// are and V tile cur is there in bf16; in the iteration every wavefront turns its rows of V tile cur+1
+// into bf16, beside the softmax of tile cur, and issues tile cur+3.
+template <int D, int NW, class Keys>
+__device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs& args, ConstI32Ptr pt,
+                                           int kt_a, int kt_mid, int kt_b, const Keys& keys,
+                                           int kv_head, char* lds, int wave, int lane) {
+  using R = Fp8Ring<D, NW>;
+  using Rows = TileRows8<D, NW>;
+  constexpr int kRound = R::kStages;
+  static_assert(kWarmTiles % kRound == 0, "the walk's head is a whole number of ring rounds");
+  if (kt_a >= kt_b) return;
+  const int half = lane >> 5;
+  const int last = kt_b - 1;
+  const int kt_u = kt_mid >= kt_b ? kt_b : kt_a + (kt_mid - kt_a) / kRound * kRound;
+  const uint32_t ring = lds_address(lds);
+  Fp8Loader<D, NW> ld;
+  ld.init(wave, lane);
+  Fp8Convert<D, NW> cv;
+  cv.init(wave, lane);
+  int page_next = 0;
+  auto next_page = [&](int i) {
+    const int t = keys.tile(min(i, last));
+    page_next = pt[__builtin_amdgcn_readfirstlane(keys.page_index(t, ld.row0))];
+  };
+  auto issue = [&](int i, int stage) {
+    ld.issue(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring, stage, wave, lane);
+  };
+  auto k_stage = [&](int s) { return lds + s * R::kTile; };
+  auto scales = [&](int s) { return lds + R::kS + s * R::kScales; };
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    next_page(kt_a + i);
+    issue(kt_a + i, i);
+  }
+  next_page(kt_a + 3);
+  f32x16 s0[2], s1[2];
+  forget(s0);
+  forget(s1);
+  ring_barrier<2 * R::kLoads>();  // tile kt_a has landed, for everyone
+  auto convert_all = [&](auto w) { cv.template convert<decltype(w)::value>(lds, 0); };
+  cv.read(lds, 0, keys.tile(kt_a), keys);
+  static_for<Fp8Convert<D, NW>::kWords>(convert_all);
+  rb.template qk<2, R::kScaleStride>(k_stage(0), scales(0), lane, s0);
+  if (kt_u > kt_a) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int f = 0; f < 32; ++f) mx = fmaxf(mx, s0[f >> 4][f & 15]);
+    rb.template update_reference<false>(mx);
+  }
+  auto round = [&](int kt, auto mask, auto spec) {
+    constexpr bool kMask = decltype(mask)::value, kSpeculate = decltype(spec)::value;
+    auto iteration = [&](auto s_const) {
+      constexpr int s = decltype(s_const)::value, s_next = (s + 1) % kRound;
+      const int cur = kt + s;
+      if (cur < last) {
+        ring_barrier_written<R::kLoads>();
+        auto at_slot = [&](auto slot) {
+          constexpr int i = decltype(slot)::value;
+          constexpr int kFirst = 6, kStep = D == 128 ? 2 : 1;
+          if constexpr (i == 1) cv.read(lds, s_next, keys.tile(cur + 1), keys);
+          if constexpr (i == Rows::kLoadSlot) {
+            asm volatile("" : "+s"(page_next));  // the page id is first needed here, not before
+            issue(cur + 3, (s + 3) % kRound);
+          }
+          if constexpr (i >= kFirst && (i - kFirst) % kStep == 0 &&
+                        (i - kFirst) / kStep < Fp8Convert<D, NW>::kWords)
+            cv.template convert<(i - kFirst) / kStep>(lds, s_next & 1);
+        };
+        const typename Rows::KSide next(rb, k_stage(s_next), scales(s_next));
+        const char* v_cur = lds + (s & 1) * (2 * R::kTile);  // + the bias in rb.v_off
+        if constexpr (s & 1)
+          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s1, s0, keys.tile(cur) * 64, half, at_slot);
+        else
+          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s0, s1, keys.tile(cur) * 64, half, at_slot);
+        // (the scalar load goes here: see run_tiles)
+        __builtin_amdgcn_sched_barrier(0);
+        next_page(cur + 4);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    static_for<kRound>(iteration);
+  };
+  int kt = kt_a;
+  const int end_u = min(kt_u, last);
+  for (; kt < end_u && kt < kt_a + kWarmTiles; kt += kRound)
+    round(kt, std::false_type{}, std::false_type{});
+  for (; __builtin_expect_with_probability(kt < end_u, 1, 0.995); kt += kRound)
+    round(kt, std::false_type{}, std::true_type{});
+  for (; kt < last; kt += kRound) round(kt, std::true_type{}, std::false_type{});
+  ring_barrier_written<R::kLoads>();  // the last V tile is there in bf16, for everyone
+  auto final_tile = [&](auto mask) {
+    constexpr bool kMask = decltype(mask)::value;
+    const typename Rows::KSide none(rb, nullptr, nullptr);
+    const char* v_last = lds + ((last - kt_a) & 1) * (2 * R::kTile);
+    if ((last - kt_a) & 1)
+      rb.template fused<kMask, false, false>(none, v_last, s1, s0, keys.tile(last) * 64, half, [](auto) {});
+    else
+      rb.template fused<kMask, false, false>(none, v_last, s0, s1, keys.tile(last) * 64, half, [](auto) {});
+  };
+  if (kt_u == kt_b)
+    final_tile(std::false_type{});
+  else
+    final_tile(std::true_type{});
+  ring_barrier<0>();
+}
+
 // Chunks: a workgroup of NW wavefronts owns NW * 32 query rows of one KV head and walks 64-key tiles,
 // as prefill_kernel does, along the tiles of its rows' windows.
+// NV: stages of the V ring, or 0 for the 8-bit cache.
 template <int D, int NW, int NV>
 __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
-  using Shape = PrefillShape<D, NW, NV>;
-  using Rows = RowBlock<D, WindowMask>;
-  __shared__ __attribute__((aligned(1024))) char lds[Shape::kLdsBytes];
-  const Ring stages{lds, lds_address(lds)};
+  constexpr bool kFp8 = NV == 0;
+  using Shape = PrefillShape<D, NW, kFp8 ? 4 : NV>;
+  using Rows = std::conditional_t<kFp8, TileRows8<D, NW>, RowBlock<D, WindowMask>>;
+  constexpr int kLdsBytes = kFp8 ? Fp8Ring<D, NW>::kLdsBytes : Shape::kLdsBytes;
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
 
   const SeqDesc* descs = args.inline_descs;
   const int seq = find_seq_slot(descs, args.n_seq, blockIdx.x);
@@ -461,7 +769,7 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int col = lane & 31, half = lane >> 5;
 
   Rows rb;
-  rb.init(fabsf(args.scale_log2), lane, Shape::kVBias);
+  rb.init(fabsf(args.scale_log2), lane, kFp8 ? wave : Shape::kVBias);
   const int wg_row0 = it.row_tile * Shape::kRowsPerWg;
   const int r = wg_row0 + wave * 32 + col;
   const bool valid = r < n_rows;
@@ -469,7 +777,8 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
   rb.mask.set(sd.prefix_len + tok, args.window);
-  Bf16Block<D>::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
+  using Block = std::conditional_t<kFp8, Fp8Block<D>, Bf16Block<D>>;
+  Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
 
   const int last_row = min(n_rows, wg_row0 + Shape::kRowsPerWg) - 1;
   const WalkKeys keys{make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,
@@ -478,10 +787,15 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int kt_end = min(keys.w.n, kt_begin + sd.tiles_per_split);
   const int kt_mid = max(kt_begin, min(kt_end, keys.w.n_full));
   ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
-  TileLoader<D, NW> loader;
-  loader.init(wave, lane);
-  run_tiles<D, NW, NV, false>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, stages, loader, wave,
-                              lane);
+  if constexpr (kFp8) {
+    run_tiles8<D, NW>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, lds, wave, lane);
+  } else {
+    const Ring stages{lds, lds_address(lds)};
+    TileLoader<D, NW> loader;
+    loader.init(wave, lane);
+    run_tiles<D, NW, NV, false>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, stages, loader,
+                                wave, lane);
+  }
 
   const bool direct = sd.n_split == 1;
   void* o_base = direct ? args.out : args.part_o;
@@ -494,10 +808,10 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const float lse = lt != 0.f ? (rb.m + fast_log2(lt)) * kLn2 : -INFINITY;
   if (valid && half == 0) l_base[(row_base + tok) * args.h_q + hq] = lse;
   if (direct && args.out_bf16)
-    write_rows<D, NW, Shape::kLdsBytes>(rb, lds, inv, static_cast<__bf16*>(o_base), row_base, tok, hq,
+    write_rows<D, NW, kLdsBytes>(rb, lds, inv, static_cast<__bf16*>(o_base), row_base, tok, hq,
                                         args.h_q, wg_row0, n_rows, wave, lane);
   else
-    write_rows<D, NW, Shape::kLdsBytes>(rb, lds, inv, static_cast<float*>(o_base), row_base, tok, hq,
+    write_rows<D, NW, kLdsBytes>(rb, lds, inv, static_cast<float*>(o_base), row_base, tok, hq,
                                         args.h_q, wg_row0, n_rows, wave, lane);
 }
 

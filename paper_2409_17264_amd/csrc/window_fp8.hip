@@ -98,7 +98,12 @@ hipError_t launch_keys(const WalkArgs& a, int grid, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_rows(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStream_t stream) {
-  if (lp.q_blocks == 2)
+  if (a.scale != nullptr) {
+    if (lp.q_blocks == 2)
+      hipLaunchKernelGGL((row_walk_kernel<D, 8, 0>), dim3(grid), dim3(512), 0, stream, a);
+    else
+      hipLaunchKernelGGL((row_walk_kernel<D, 4, 0>), dim3(grid), dim3(256), 0, stream, a);
+  } else if (lp.q_blocks == 2)
     hipLaunchKernelGGL((row_walk_kernel<D, 8, 4>), dim3(grid), dim3(512), 0, stream, a);
   else if (lp.paired)
     hipLaunchKernelGGL((row_walk_kernel<128, 4, 2>), dim3(grid), dim3(256), 0, stream, a);
@@ -171,9 +176,8 @@ bool window_of(int32_t keys, int32_t sinks, bool optional, Window& w) {
 }
 
 Plan walk_plan(const std::vector<SeqInput>& seqs, int h_q, int h_kv, int d, size_t budget,
-               const Window& w, bool fp8) {
-  return make_plan(seqs.data(), (int)seqs.size(), h_q, h_kv, d, current_num_cus(), budget, w,
-                   fp8 ? INT64_MAX : 32);
+               const Window& w) {
+  return make_plan(seqs.data(), (int)seqs.size(), h_q, h_kv, d, current_num_cus(), budget, w);
 }
 
 size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32_t batch,
@@ -192,8 +196,7 @@ size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32
     row += chunk_len[b];
     if (row > INT32_MAX) return 0;
   }
-  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w, optional)
-      .workspace_bytes();
+  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w).workspace_bytes();
 }
 
 // A call on either cache.  `kv` describes its pools, `scale` is null for the bf16 one; `alloc`: asked
@@ -231,8 +234,7 @@ int walk_attn(const void* q, const medha_kv_cache* kv, const void* scale, const 
     if (row > INT32_MAX) return MEDHA_ERR_INVALID_ARG;
   }
   const Plan plan = walk_plan(seqs, num_q_heads, kv->num_kv_heads, kv->head_dim,
-                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window,
-                              scale != nullptr);
+                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window);
   if (alloc) {
     workspace_bytes = plan.workspace_bytes();
     workspace = alloc(workspace_bytes, context);
