@@ -21,6 +21,7 @@
 
 namespace medha {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
@@ -82,22 +83,44 @@ struct PageRead {
   }
 };
 
-__device__ __forceinline__ void async_load4(const void* gptr, uint32_t lds_addr_uniform) {
+__device__ __forceinline__ void async_load4(const void* base_uniform, uint32_t lane_off,
+                                            uint32_t lds_addr_uniform) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(lds_addr_uniform), "v"(lane_off), "s"(base_uniform)
+               : "m0", "memory");
+}
+
+__device__ __forceinline__ void async_load4_at(const void* gptr, uint32_t lds_addr_uniform) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :
                : "s"(lds_addr_uniform), "v"(gptr)
                : "m0", "memory");
 }
 
-// ---------------------------------------------------------------- a block of 32 keys, bf16 cache
+// ---------------------------------------------------------------- blocks of 32 keys, bf16 cache
 
 template <int D>
 struct Bf16Block {
   using G = DecodeGeom<D>;
   using Rows = RowBlock<D, WindowMask>;
-  static constexpr int kBytes = G::kBlockBytes;   // ring stage
-  static constexpr int kScratchBytes = 0;         // per wavefront, beside the ring
+  static constexpr int kBytes = G::kBlockBytes;  // ring stage: K, V
   static constexpr int kLoads = G::kLoadsPerBlock;
+  static constexpr int kPerPage = kPageSize / G::kRowsPerInstr;
+  uint32_t k_off[kPerPage], v_off[kPerPage];  // of a whole page, within the (page, KV head) block
+  int r_in, pos, half;
+
+  __device__ __forceinline__ void init(int lane) {
+    r_in = lane / G::kChunksPerRow;
+    pos = lane % G::kChunksPerRow;
+    half = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < kPerPage; ++j) {
+      const int r = j * G::kRowsPerInstr + r_in;
+      k_off[j] = r * (D * 2) + Swz<D>::k(r, pos) * 16;
+      v_off[j] = r * (D * 2) + Swz<D>::v(r, pos) * 16;
+    }
+  }
 
   __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
                                                 bool valid, int half) {
@@ -111,29 +134,34 @@ struct Bf16Block {
     }
   }
 
-  __device__ static __forceinline__ void issue(const WalkArgs& args, ConstI32Ptr pt, const KeyWalk& w,
-                                               int key0, int kv_head, uint32_t stage, int lane) {
-    const int r_in = lane / G::kChunksPerRow, pos = lane % G::kChunksPerRow;
+  // Loads the block at key0 into `stage`; the ids of its two pages are page[0] and page[1].  WHOLE: all
+  // of its keys are read.
+  template <bool WHOLE, bool kOnce>
+  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyWalk& w,
+                                        int key0, int kv_head, uint32_t stage) const {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
+      const int64_t block = ((int64_t)page[p] * args.h_kv + kv_head) * (kPageSize * D * 2);
+      const char *kp = args.k_pool + block, *vp = args.v_pool + block;
       const PageRead pr(w, key0 + p * kPageSize);
-      const int page = pt[__builtin_amdgcn_readfirstlane(pr.page_index)];
-      const int64_t base = ((int64_t)page * args.h_kv + kv_head) * (kPageSize * D * 2);
 #pragma unroll
-      for (int j = 0; j < kPageSize / G::kRowsPerInstr; ++j) {
-        const int r = j * G::kRowsPerInstr + r_in, row = p * kPageSize + r;
-        const int64_t off = base + pr.slot(r) * (D * 2);
+      for (int j = 0; j < kPerPage; ++j) {
+        uint32_t ko = k_off[j], vo = v_off[j];
+        if (!WHOLE) {
+          const int r = j * G::kRowsPerInstr + r_in, slot = pr.slot(r);
+          ko = slot * (D * 2) + Swz<D>::k(r, pos) * 16;
+          vo = slot * (D * 2) + Swz<D>::v(r, pos) * 16;
+        }
         const uint32_t to = stage + (p * kPageSize + j * G::kRowsPerInstr) * (D * 2);
-        async_stream16<false>(args.k_pool + off + Swz<D>::k(row, pos) * 16, to);
-        async_stream16<false>(args.v_pool + off + Swz<D>::v(row, pos) * 16, to + G::kHalfBytes);
+        async_load16<kOnce>(kp, ko, to);
+        async_load16<kOnce>(vp, vo, to + G::kHalfBytes);
       }
     }
   }
 
   template <bool MASK>
-  __device__ static __forceinline__ void step(Rows& rb, const char* stage, char*, const KeyWalk&,
-                                              int key0, int lane) {
-    rb.template step<1, MASK>(stage, stage + G::kHalfBytes, key0, lane >> 5);
+  __device__ __forceinline__ void step(Rows& rb, const char* stage, int key0) const {
+    rb.template step<1, MASK>(stage, stage + G::kHalfBytes, key0, half);
   }
 };
 
@@ -223,11 +251,44 @@ struct Fp8Block {
   using Rows = Rows8<D>;
   static constexpr int kHalfBytes = 32 * D;
   static constexpr int kBytes = 2 * kHalfBytes + 256;   // K, V, and 64 lanes' worth of scale bytes
-  static constexpr int kScratchBytes = 32 * D * 2;      // the block's values in bf16
   static constexpr int kChunksPerRow = D / 16;
   static constexpr int kRowsPerInstr = 64 / kChunksPerRow;  // 8 or 16
-  static constexpr int kInstr = 32 / kRowsPerInstr;
-  static constexpr int kLoads = 2 * kInstr + 1;
+  static constexpr int kPerPage = kPageSize / kRowsPerInstr;
+  static constexpr int kLoads = 4 * kPerPage + 1;
+  uint32_t k_off[kPerPage], v_off[kPerPage];
+  int k8_off[2 * Rows::kParts];    // this lane's pieces of key row lane % 32
+  int vt_off[Rows::kDBlocks];      // its place in the transposing reads of a 16-key slice
+  int ks_off, r_in, pos, lane, half;
+
+  // 16-byte chunk of a V row: the 8 rows x 32 columns that 32 lanes read at a time hit all banks.
+  __device__ static __forceinline__ int vswz(int row, int chunk) {
+    const int g = D == 128 ? ((row >> 1) & 1) * 2 + ((row >> 3) & 1) * 4 : ((row >> 3) & 1) * 2;
+    return chunk ^ g;
+  }
+
+  __device__ __forceinline__ void init(int ln) {
+    lane = ln;
+    half = ln >> 5;
+    r_in = ln / kChunksPerRow;
+    pos = ln % kChunksPerRow;
+#pragma unroll
+    for (int j = 0; j < kPerPage; ++j) {
+      const int r = j * kRowsPerInstr + r_in;
+      k_off[j] = r * D + swz8<D>(r, pos) * 16;
+      v_off[j] = r * D + vswz(r, pos) * 16;
+    }
+    const int col = ln & 31;
+#pragma unroll
+    for (int i = 0; i < 2 * Rows::kParts; ++i)
+      k8_off[i] = col * D + swz8<D>(col, (i >> 1) * 4 + half * 2 + (i & 1)) * 16;
+    ks_off = (col >> 4) * kScaleBytesPerPage + (col & 15);
+    // keys of a slice in the order of P^T's registers: 4*half + 0..3, then the same + 8
+    const int l16 = ln & 15, dhalf = (ln >> 4) & 1, j = l16 >> 1;
+    const int row = (j & 4) * 2 + 4 * half + (j & 3);
+#pragma unroll
+    for (int db = 0; db < Rows::kDBlocks; ++db)
+      vt_off[db] = row * D + vswz(row, 2 * db + dhalf) * 16 + (l16 & 1) * 8;
+  }
 
   __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
                                                 bool valid, int half) {
@@ -242,56 +303,95 @@ struct Fp8Block {
     rb.set_q(raw);
   }
 
-  __device__ static __forceinline__ void issue(const WalkArgs& args, ConstI32Ptr pt, const KeyWalk& w,
-                                               int key0, int kv_head, uint32_t stage, int lane) {
-    const int r_in = lane / kChunksPerRow, pos = lane % kChunksPerRow;
-    int64_t page_head[2];
+  template <bool WHOLE, bool kOnce>
+  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyWalk& w,
+                                        int key0, int kv_head, uint32_t stage) const {
+    int64_t block[2];
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
+      block[p] = (int64_t)page[p] * args.h_kv + kv_head;
+      const char* kp = args.k_pool + block[p] * (kPageSize * D);
+      const char* vp = args.v_pool + block[p] * (kPageSize * D);
       const PageRead pr(w, key0 + p * kPageSize);
-      const int page = pt[__builtin_amdgcn_readfirstlane(pr.page_index)];
-      page_head[p] = (int64_t)page * args.h_kv + kv_head;
 #pragma unroll
-      for (int j = 0; j < kPageSize / kRowsPerInstr; ++j) {
-        const int r = j * kRowsPerInstr + r_in, row = p * kPageSize + r;
-        const int64_t off = page_head[p] * (kPageSize * D) + pr.slot(r) * D;
+      for (int j = 0; j < kPerPage; ++j) {
+        uint32_t ko = k_off[j], vo = v_off[j];
+        if (!WHOLE) {
+          const int r = j * kRowsPerInstr + r_in, slot = pr.slot(r);
+          ko = slot * D + swz8<D>(r, pos) * 16;
+          vo = slot * D + vswz(r, pos) * 16;
+        }
         const uint32_t to = stage + (p * kPageSize + j * kRowsPerInstr) * D;
-        async_stream16<false>(args.k_pool + off + swz8<D>(row, pos) * 16, to);
-        async_stream16<false>(args.v_pool + off + pos * 16, to + kHalfBytes);
+        async_load16<kOnce>(kp, ko, to);
+        async_load16<kOnce>(vp, vo, to + kHalfBytes);
       }
     }
     // (lanes 0-7 and 8-15 hold the two pages' 32 bytes, the others repeat them)
-    const int64_t ph = (lane & 8) ? page_head[1] : page_head[0];
-    async_load4(args.scale + ph * kScaleBytesPerPage + (lane & 7) * 4, stage + 2 * kHalfBytes);
+    const int64_t b = (lane & 8) ? block[1] : block[0];
+    async_load4_at(args.scale + b * kScaleBytesPerPage + (lane & 7) * 4, stage + 2 * kHalfBytes);
   }
 
+  // The values stay 8 bits wide until the transposing reads have them in registers.  There they
+  // become bf16 without their scales, which differ from key to key: the scale of key t is a factor of
+  // P[t] instead, a power of two, so nothing is rounded that would not have been.  (With a scale of
+  // 2^-117 a probability below 2^-9 is lost to bf16's range: values below 2^-109.)
   template <bool MASK>
-  __device__ static __forceinline__ void step(Rows& rb, const char* stage, char* scratch,
-                                              const KeyWalk& w, int key0, int lane) {
+  __device__ __forceinline__ void step(Rows& rb, const char* stage, int key0) const {
     const char* scales = stage + 2 * kHalfBytes;
-    // the values become bf16, exactly, where the transposing reads expect them
-    const int r_in = lane / kChunksPerRow, pos = lane % kChunksPerRow;
+    const char* v_lds = stage + kHalfBytes;
+    i32x2 raw[2][Rows::kDBlocks];
 #pragma unroll
-    for (int j = 0; j < kInstr; ++j) {
-      const int row = j * kRowsPerInstr + r_in;
-      int slot = row & 15;
-      if (MASK) slot = PageRead(w, key0 + (j * kRowsPerInstr & 16)).slot(slot);
-      const uint32_t byte = (uint8_t)scales[(row >> 4) * kScaleBytesPerPage + kPageSize + slot];
-      const uint4 raw = *reinterpret_cast<const uint4*>(stage + kHalfBytes + j * 1024 + lane * 16);
-      char* to = scratch + row * (D * 2);
-      *reinterpret_cast<uint4*>(to + Swz<D>::v(row, 2 * pos) * 16) =
-          dequantise8(make_uint2(raw.x, raw.y), byte);
-      *reinterpret_cast<uint4*>(to + Swz<D>::v(row, 2 * pos + 1) * 16) =
-          dequantise8(make_uint2(raw.z, raw.w), byte);
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int db = 0; db < Rows::kDBlocks; ++db)
+        raw[g][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (i32x2 __attribute__((address_space(3)))*)(v_lds + g * 16 * D + vt_off[db]));
+    uint32_t vs[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      vs[i] = *reinterpret_cast<const uint32_t*>(scales + (i >> 1) * kScaleBytesPerPage + kPageSize +
+                                                 (i & 1) * 8 + half * 4);
+    const int ks = (uint8_t)scales[ks_off];
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+    for (int part = 0; part < Rows::kParts; ++part) {
+      const i32x4 x = *reinterpret_cast<const i32x4*>(stage + k8_off[2 * part]);
+      const i32x4 y = *reinterpret_cast<const i32x4*>(stage + k8_off[2 * part + 1]);
+      const i32x8 a = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rb.hi[part], s, 0, 0, 0, ks, 0, rb.hi_scale);
+      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rb.lo[part], s, 0, 0, 0, ks, 0, rb.lo_scale);
     }
-    asm volatile("" ::: "memory");  // (one wavefront's LDS accesses stay in order)
-    f32x16 s[1];
-    rb.template qk<1>(stage, scales, lane, s);
-    bf16x8 vop[2][Rows::kDBlocks];
-    rb.read_v_slice(scratch, 0, vop[0]);
-    rb.read_v_slice(scratch, 1, vop[1]);
-    rb.template softmax_pv<1, MASK>(s, scratch, vop, key0, lane >> 5);
-    asm volatile("" ::: "memory");
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      if (MASK) s[e] = rb.mask.sees(key0 + 8 * (e >> 2) + 4 * half + (e & 3)) ? s[e] : -INFINITY;
+      mx = fmaxf(mx, s[e]);
+    }
+    const float m_use = rb.template update_reference<MASK>(mx);
+    float ls = 0.f;
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x8 pe;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float pr = rb.prob(s[8 * g + e], m_use);
+        ls += pr;
+        const uint32_t byte = (vs[2 * g + (e >> 2)] >> (8 * (e & 3))) & 0xffu;
+        pe[e] = pr * __builtin_bit_cast(float, byte << 23);
+        // (a key that is not seen weighs nothing, whatever stands in the scale's place)
+        if (MASK) pe[e] = pr > 0.f ? pe[e] : 0.f;
+      }
+      const bf16x8 pv = __builtin_convertvector(pe, bf16x8);
+#pragma unroll
+      for (int db = 0; db < Rows::kDBlocks; ++db) {
+        const uint2 lo = dequantise4(raw[g][db][0], 1.f), hi = dequantise4(raw[g][db][1], 1.f);
+        const bf16x8 v = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+        rb.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pv, rb.o[db], 0, 0, 0);
+      }
+    }
+    rb.add_to_sum(ls);
   }
 };
 
@@ -305,10 +405,26 @@ __device__ __forceinline__ void store_out(void* to, int64_t i, const f32x4& v, b
     store4(static_cast<float*>(to) + i, v);
 }
 
+// The pages of a wavefront's blocks, 32 blocks at a time: one vector load, two lanes a block.  (Read
+// block by block, each pair of ids is a trip to memory that the block's own loads wait for.)
+struct BlockPages {
+  int ids;
+  // blocks b, b + kWaves, ... of the walk
+  __device__ __forceinline__ void load(const int32_t* table, const KeyWalk& w, int b, int lane) {
+    const int at = min(b + (lane >> 1) * kWaves, w.n - 1);
+    ids = table[PageRead(w, w.tile(at) * 32 + (lane & 1) * kPageSize).page_index];
+  }
+  __device__ __forceinline__ void get(int i, int (&page)[2]) const {
+    page[0] = __builtin_amdgcn_readlane(ids, 2 * i);
+    page[1] = __builtin_amdgcn_readlane(ids, 2 * i + 1);
+  }
+};
+
+// STAGES blocks of every wavefront are in flight while it waits for the first of them.
 // (launched with 256 threads; the bound: see decode_kernel)
 template <int D, class Block, int STAGES>
 __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs args) {
-  constexpr int kWaveBytes = STAGES * Block::kBytes + Block::kScratchBytes;
+  constexpr int kWaveBytes = STAGES * Block::kBytes;
   constexpr int kCombineBytes = kWaves * 32 * (D + 2) * 4;
   __shared__ __attribute__((aligned(1024))) char
       lds[kWaves * kWaveBytes > kCombineBytes ? kWaves * kWaveBytes : kCombineBytes];
@@ -318,51 +434,71 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
   const int lane = threadIdx.x & 63;
   const int seq = find_seq_slot(descs, args.n_seq, blockIdx.x);
   const SeqDesc sd = uniform(descs[seq]);
-  const KeySplitItem it =
-      key_split_item(sd, blockIdx.x - sd.work_start, args.h_kv * sd.n_row_tiles);
-  const int split = it.split;
-  const int kv_head = it.kv_head / sd.n_row_tiles, row0 = it.kv_head % sd.n_row_tiles * 32;
+  const KeySplitItem it = key_split_item(sd, blockIdx.x - sd.work_start, args.h_kv);
+  const int split = it.split, kv_head = it.kv_head;
 
   const int gqa = args.h_q / args.h_kv;
-  const int n_rows = min(32, sd.chunk_len * gqa - row0);
+  const int n_rows = sd.chunk_len * gqa;  // <= 32
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
+
+  const KeyWalk walk = make_walk(sd.prefix_len, sd.prefix_len + sd.chunk_len - 1, args.window, 32);
+  const int b_first = split * sd.tiles_per_split * kWaves + wave;
+  const int b_end = min(walk.n, (split + 1) * sd.tiles_per_split * kWaves);
+  const int n_blocks = b_end > b_first ? (b_end - b_first + kWaves - 1) / kWaves : 0;
+  const int n_full = min(n_blocks, max(0, walk.n_full - b_first + kWaves - 1) / kWaves);
+  BlockPages pages;
+  pages.load(args.page_table + sd.pt_off, walk, b_first, lane);
 
   Rows rb;
   rb.init(fabsf(args.scale_log2), lane);
   const bool valid = col < n_rows;
-  const int rr = row0 + (valid ? col : n_rows - 1);
+  const int rr = valid ? col : n_rows - 1;
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
   rb.mask.set(sd.prefix_len + tok, args.window);
   Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
+  Block block;
+  block.init(lane);
 
-  const KeyWalk walk = make_walk(sd.prefix_len + row0 / gqa, sd.prefix_len + (row0 + n_rows - 1) / gqa,
-                                 args.window, 32);
-  const int b_begin = split * sd.tiles_per_split * kWaves;
-  const int b_end = min(walk.n, b_begin + sd.tiles_per_split * kWaves);
-  ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
   char* ring = lds + wave * kWaveBytes;
-  char* scratch = ring + STAGES * Block::kBytes;
   const uint32_t ring_lds = lds_address(lds) + wave * kWaveBytes;
-  auto issue = [&](int b, int st) {
-    Block::issue(args, pt, walk, walk.tile(b) * 32, kv_head, ring_lds + st * Block::kBytes, lane);
+  // block i of the wavefront
+  auto issue = [&](int i, int st) {
+    if (i > 0 && i % 32 == 0)
+      pages.load(args.page_table + sd.pt_off, walk, b_first + i * kWaves, lane);
+    int page[2];
+    pages.get(i & 31, page);
+    const int key0 = walk.tile(b_first + i * kWaves) * 32;
+    const uint32_t to = ring_lds + st * Block::kBytes;
+    if (i < n_full)
+      block.template issue<true, true>(args, page, walk, key0, kv_head, to);
+    else
+      block.template issue<false, true>(args, page, walk, key0, kv_head, to);
   };
-  if (b_begin + wave < b_end) issue(b_begin + wave, 0);
-  int st = 0;
-  for (int b = b_begin + wave; b < b_end; b += kWaves, st ^= 1) {
-    if (b + kWaves < b_end) {
-      issue(b + kWaves, st ^ 1);
-      wait_vmcnt<Block::kLoads>();  // the younger block may still fly
+  int st_issue = 0, st = 0;
+  auto next = [](int x) { return x + 1 == STAGES ? 0 : x + 1; };
+  for (int i = 0; i < STAGES - 1 && i < n_blocks; ++i) {
+    issue(i, st_issue);
+    st_issue = next(st_issue);
+  }
+  for (int i = 0; i < n_blocks; ++i) {
+    if (i + STAGES - 1 < n_blocks) {
+      issue(i + STAGES - 1, st_issue);
+      st_issue = next(st_issue);
+      wait_vmcnt<(STAGES - 1) * Block::kLoads>();  // the younger blocks may still fly
     } else {
       wait_vmcnt<0>();
     }
     const char* stage = ring + st * Block::kBytes;
-    if (b < walk.n_full)
-      Block::template step<false>(rb, stage, scratch, walk, walk.tile(b) * 32, lane);
+    const int key0 = walk.tile(b_first + i * kWaves) * 32;
+    if (i < n_full)
+      block.template step<false>(rb, stage, key0);
     else
-      Block::template step<true>(rb, stage, scratch, walk, walk.tile(b) * 32, lane);
-    // every LDS read of the stage has returned (its data fed the matrix cores)
+      block.template step<true>(rb, stage, key0);
+    st = next(st);
+    // every LDS read of the stage has returned before a load refills it
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 
   // Combine the 4 wavefronts' (m, l, O) over their disjoint keys through LDS.
@@ -413,8 +549,7 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
       acc += *reinterpret_cast<const f32x4*>(sm_o + (w * 32 + rl) * D + d4 * 4) * a;
     }
     const float inv = lt_all != 0.f ? 1.f / lt_all : 0.f;
-    const int r = row0 + rl;
-    const int64_t orow = (row_base + r / gqa) * args.h_q + kv_head * gqa + r % gqa;
+    const int64_t orow = (row_base + rl / gqa) * args.h_q + kv_head * gqa + rl % gqa;
     store_out(o_base, orow * D + d4 * 4, acc * inv, as_bf16);
     if (d4 == 0) l_base[orow] = lt_all != 0.f ? (mm + fast_log2(lt_all)) * kLn2 : -INFINITY;
   }
@@ -438,14 +573,6 @@ struct WalkKeys {
 };
 
 // ---------------------------------------------------------------- row-split, 8-bit cache
-
-__device__ __forceinline__ void async_load4(const void* base_uniform, uint32_t lane_off,
-                                            uint32_t lds_addr_uniform) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
-               :
-               : "s"(lds_addr_uniform), "v"(lane_off), "s"(base_uniform)
-               : "m0", "memory");
-}
 
 // As ring_barrier(), and this wavefront's LDS writes are done.
 template <int N>
