@@ -88,9 +88,15 @@ int move_tokens(Kernel kernel, const void* k_rows, const void* v_rows, const med
 // ------------------------------------------------------------------ attention
 
 template <int D>
-hipError_t launch_keys(const WalkArgs& a, int grid, hipStream_t stream) {
+hipError_t launch_keys(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStream_t stream) {
+  int64_t steps = 0;
+  for (int i = 0; i < a.n_seq; ++i)
+    steps = std::max<int64_t>(steps, std::min<int64_t>(a.inline_descs[i].tiles_per_split,
+                                                       kv_tiles_of(a.inline_descs[i], lp.shape)));
   if (a.scale != nullptr)
     hipLaunchKernelGGL((key_walk_kernel<D, Fp8Block<D>, 2>), dim3(grid), dim3(kThreads), 0, stream, a);
+  else if (steps <= kShortWalkTiles && grid > lp.num_cus)
+    hipLaunchKernelGGL((key_walk_kernel<D, Bf16Block<D>, 1>), dim3(grid), dim3(kThreads), 0, stream, a);
   else
     hipLaunchKernelGGL((key_walk_kernel<D, Bf16Block<D>, 2>), dim3(grid), dim3(kThreads), 0, stream, a);
   return hipGetLastError();
@@ -147,7 +153,7 @@ hipError_t launch_walks(const LaunchPlan& lp, WalkArgs& a, hipStream_t stream) {
       max_split = std::max(max_split, sd.n_split);
     }
     if (slot1 == slot0) continue;
-    hipError_t e = lp.key_split ? launch_keys<D>(a, slot1 - slot0, stream)
+    hipError_t e = lp.key_split ? launch_keys<D>(lp, a, slot1 - slot0, stream)
                                 : launch_rows<D>(lp, a, slot1 - slot0, stream);
     if (e != hipSuccess) return e;
     if (max_split == 1) continue;
