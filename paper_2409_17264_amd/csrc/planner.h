@@ -166,14 +166,16 @@ inline double makespan(std::vector<WalkGroup>& groups, int64_t machines, const W
   return end;
 }
 
-// Tiles of the longest walk of a sequence's row tiles: all its keys, or with a window at most the
-// tiles that a row tile's windows and the first tokens can touch.
+// Visits of the longest walk of a sequence's row tiles: all its tiles, or with a window at most the
+// tiles that a row tile's windows and the first tokens can touch (where these overlap, twice).
 inline int64_t kv_tiles_of(const SeqDesc& sd, const ModeShape& sh) {
   const int64_t all = std::max<int64_t>(1, ceil_div((int64_t)sd.kv_len, sh.tile_keys));
   if (sd.kv_len <= sh.window.keys) return all;
   const int64_t tokens = std::min<int64_t>(sd.chunk_len, (sh.rows_per_wg + sh.gqa - 2) / sh.gqa + 1);
+  const int64_t first = std::min(all, ceil_div(sh.window.sinks, sh.tile_keys));
   const int64_t reach = sh.window.keys + tokens - 1;  // keys from the first row's window to the last row
-  return std::min(all, (reach - 1) / sh.tile_keys + 2 + ceil_div(sh.window.sinks, sh.tile_keys));
+  return std::min(all + std::min(first, tokens / sh.tile_keys + 2),
+                  (reach - 1) / sh.tile_keys + 2 + first);
 }
 
 // Tiles that row tile rt of a sequence walks.

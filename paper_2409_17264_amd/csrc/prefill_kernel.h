@@ -120,10 +120,19 @@ struct TileGeom {
 // clamped to the last one: they are masked, but must be finite.
 typedef const int32_t __attribute__((address_space(4))) * ConstI32Ptr;
 
+// Which keys a row sees: those up to its limit.
+struct CausalMask {
+  int limit;  // last visible key index of the lane's row
+  __device__ __forceinline__ bool sees(int t) const { return t <= limit; }
+};
+
 // The keys of a walk over all of a sequence's: tile i of the walk is its tile i.
 struct AllKeys {
   int kv_total;
   __device__ __forceinline__ int tile(int i) const { return i; }
+  __device__ __forceinline__ int key0(int t) const { return t * 64; }
+  // what a row sees of tile t
+  __device__ __forceinline__ void show(CausalMask&, int) const {}
   // whether every key of 64-key tile t is read
   __device__ __forceinline__ bool whole(int t) const { return (t + 1) * 64 <= kv_total; }
   // page of the keys from `row` on (16 or fewer, of one page); slot of one of them
@@ -210,12 +219,6 @@ template <int N, class F>
 __device__ __forceinline__ void static_for(F& f) {
   static_for_impl(std::make_integer_sequence<int, N>{}, f);
 }
-
-// Which keys a row sees: those up to its limit.
-struct CausalMask {
-  int limit;  // last visible key index of the lane's row
-  __device__ __forceinline__ bool sees(int t) const { return t <= limit; }
-};
 
 template <int D, class Mask = CausalMask>
 struct RowBlock {
@@ -782,11 +785,12 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
         };
         const typename Rows::KSide k_next(rb, ring.base + ((s + 1) % R::kK) * kTile);
         const char* v_cur = ring.base + (s % R::kV) * kTile;  // + the bias in rb.v_off
+        if constexpr (kMask) keys.show(rb.mask, keys.tile(cur));
         if constexpr (s & 1)
-          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, keys.tile(cur) * 64, half,
+          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, keys.key0(keys.tile(cur)), half,
                                                      issue_loads);
         else
-          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s0, s1, keys.tile(cur) * 64, half,
+          rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s0, s1, keys.key0(keys.tile(cur)), half,
                                                      issue_loads);
         // The scalar load of the next page id goes HERE, after the tile's last LDS read has
         // been consumed and before the barrier: scalar loads and LDS reads share one
@@ -820,10 +824,13 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
   auto final_tile = [&](auto mask) {
     constexpr bool kMask = decltype(mask)::value;
     const char* v_last = ring.base + ((last - kt_a) % R::kV) * kTile;  // + the bias in rb.v_off
+    if constexpr (kMask) keys.show(rb.mask, keys.tile(last));
     if ((last - kt_a) & 1)
-      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s1, s0, keys.tile(last) * 64, half, [](auto) {});
+      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s1, s0, keys.key0(keys.tile(last)), half,
+                                                   [](auto) {});
     else
-      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s0, s1, keys.tile(last) * 64, half, [](auto) {});
+      rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s0, s1, keys.key0(keys.tile(last)), half,
+                                                   [](auto) {});
   };
   if (kt_u == kt_b)
     final_tile(std::false_type{});

@@ -13,20 +13,25 @@ struct Window {
   int32_t sinks = 0;
 };
 
-// The tiles of `tile_keys` keys that rows at positions [p_a, p_b] see, as one row of n indexes.
-// Their windows reach keys [lo, end); before lo they see keys [0, first).  Softmax attention does
-// not care for the order of its keys, so the tiles that every row sees in full come first
-// (n_full of them, which need no mask), behind them the other tiles up to the rows' own, the first
-// tokens' tiles and the left edge of the windows:
+// The tiles of `tile_keys` keys that rows at positions [p_a, p_b] see, as one row of n visits.  A
+// visit shows a row either the window's keys of its tile, or its first tokens that no window of the
+// row reaches: every visit's keys are one interval for each row, and no key is shown twice.  (A tile
+// that holds keys of both kinds is visited twice.)  The windows reach keys [lo, end), the visits for
+// first tokens show keys [0, first).  Softmax attention does not care for the order of its keys, so
+// the tiles that every row's window covers come first (n_full of them, which need no mask), behind
+// them the other tiles up to the rows' own, the first tokens' and the left edge of the windows:
 //     [u0, w1)  [0, s1)  [w0, u0)
 struct KeyWalk {
   int32_t lo, end, first;
   int32_t w0, w1, u0, s1;
   int32_t n, n_full;
 
+  __host__ __device__ __forceinline__ bool first_tokens(int i) const {
+    return (uint32_t)(i - (w1 - u0)) < (uint32_t)s1;
+  }
   __host__ __device__ __forceinline__ int tile(int i) const {
-    const int from_u0 = u0 + i, rest = i - (w1 - u0);
-    return rest < 0 ? from_u0 : rest < s1 ? rest : w0 + rest - s1;
+    const int rest = i - (w1 - u0);
+    return rest < 0 ? u0 + i : rest < s1 ? rest : w0 + rest - s1;
   }
 };
 
@@ -37,12 +42,11 @@ __host__ __device__ inline KeyWalk make_walk(int32_t p_a, int32_t p_b, const Win
   KeyWalk k;
   k.lo = at_least_0(p_a - win.keys + 1);
   k.end = p_b + 1;
-  k.first = win.sinks < k.lo ? win.sinks : k.lo;
+  const int32_t all_see = at_least_0(p_b - win.keys + 1);  // from here on every row sees, up to p_a
+  k.first = win.sinks < all_see ? win.sinks : all_see;
   k.w0 = k.lo / tile_keys;
   k.w1 = (k.end - 1) / tile_keys + 1;
-  const int32_t s1 = k.first > 0 ? (k.first - 1) / tile_keys + 1 : 0;
-  k.s1 = s1 < k.w0 ? s1 : k.w0;
-  const int32_t all_see = at_least_0(p_b - win.keys + 1);  // from here on every row sees, up to p_a
+  k.s1 = k.first > 0 ? (k.first - 1) / tile_keys + 1 : 0;
   const int32_t u0 = all_see > 0 ? (all_see - 1) / tile_keys + 1 : 0, u1 = (p_a + 1) / tile_keys;
   k.n_full = u1 > u0 ? u1 - u0 : 0;
   k.u0 = k.n_full > 0 ? u0 : k.w0;

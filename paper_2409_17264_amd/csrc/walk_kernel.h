@@ -6,8 +6,8 @@
 // wavefront streams its blocks HBM -> LDS with asynchronous 16-byte loads into a private ring, so
 // the loop has no workgroup barrier.
 //
-// Only keys that some row of the workgroup sees are read: what lies between the first tokens and
-// the windows stands in for a key that is seen, and is masked.  The pages there may be gone.
+// Only keys that some row of the workgroup sees are read.  The pages between the first tokens and the
+// windows may be gone.
 #pragma once
 
 #include <type_traits>
@@ -46,41 +46,29 @@ struct WalkArgs {
 };
 static_assert(sizeof(WalkArgs) <= 4096, "kernel argument block too large");
 
+// What a row sees in a visit: the keys of one interval.
 struct WindowMask {
-  int limit;  // the row's position
-  int lo;     // first key of its window
-  int sinks;
-  __device__ __forceinline__ bool sees(int t) const {
-    return (t <= limit) & ((t >= lo) | (t < sinks));
-  }
-  __device__ __forceinline__ void set(int position, const Window& w) {
-    limit = position;
-    lo = position - w.keys + 1;
-    sinks = w.sinks;
+  int from, to;
+  int position;   // of the row
+  Window window;  // (wave-uniform)
+  __device__ __forceinline__ bool sees(int t) const { return (t >= from) & (t <= to); }
+  __device__ __forceinline__ void visit(bool first_tokens) {
+    const int reach = max(0, position - window.keys + 1);
+    from = first_tokens ? 0 : reach;
+    to = first_tokens ? min(window.sinks, reach) - 1 : position;
   }
 };
 
-// Where the 16 keys of one page's worth of a walk, from key g (a multiple of 16) on, are read from.
-struct PageRead {
-  int page_index;    // in the sequence's table (wave-uniform)
-  int g, lo, end, first;
-  bool sinks_only;   // the group ends before the windows begin, but holds first tokens
-  __device__ __forceinline__ PageRead(const KeyWalk& w, int group) {
-    g = group;
-    lo = w.lo;
-    end = w.end;
-    first = w.first;
-    const bool below = g + kPageSize <= lo;
-    sinks_only = below && g < first;
-    const int t = below && !sinks_only ? lo : min(g, end - 1);
-    page_index = t >> 4;
-  }
-  // Slot to read for key g + r: its own if some row sees it, that of a key that is seen otherwise.
-  __device__ __forceinline__ int slot(int r) const {
-    const int t = g + r;
-    const int near = sinks_only ? first - 1 : max(t, lo);
-    return min(t < first ? t : near, end - 1) & (kPageSize - 1);
-  }
+// Where the keys of a visit are read from: keys that no row sees in it stand for the nearest one that
+// some row does (they are masked, but have to be finite, and their pages may be gone).
+struct KeyRange {
+  int from, to;
+  __device__ __forceinline__ KeyRange(const KeyWalk& w, bool first_tokens)
+      : from(first_tokens ? 0 : w.lo), to((first_tokens ? w.first : w.end) - 1) {}
+  __device__ __forceinline__ int key(int t) const { return min(max(t, from), to); }
+  // the page, in the sequence's table, of the 16 keys from t on (a multiple of 16)
+  __device__ __forceinline__ int page_index(int t) const { return key(t) >> 4; }
+  __device__ __forceinline__ bool whole(int t, int n) const { return t >= from && t + n - 1 <= to; }
 };
 
 __device__ __forceinline__ void async_load4(const void* base_uniform, uint32_t lane_off,
@@ -137,18 +125,17 @@ struct Bf16Block {
   // Loads the block at key0 into `stage`; the ids of its two pages are page[0] and page[1].  WHOLE: all
   // of its keys are read.
   template <bool WHOLE, bool kOnce>
-  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyWalk& w,
+  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyRange& range,
                                         int key0, int kv_head, uint32_t stage) const {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int64_t block = ((int64_t)page[p] * args.h_kv + kv_head) * (kPageSize * D * 2);
       const char *kp = args.k_pool + block, *vp = args.v_pool + block;
-      const PageRead pr(w, key0 + p * kPageSize);
 #pragma unroll
       for (int j = 0; j < kPerPage; ++j) {
         uint32_t ko = k_off[j], vo = v_off[j];
         if (!WHOLE) {
-          const int r = j * G::kRowsPerInstr + r_in, slot = pr.slot(r);
+          const int r = j * G::kRowsPerInstr + r_in, slot = range.key(key0 + p * kPageSize + r) & 15;
           ko = slot * (D * 2) + Swz<D>::k(r, pos) * 16;
           vo = slot * (D * 2) + Swz<D>::v(r, pos) * 16;
         }
@@ -304,7 +291,7 @@ struct Fp8Block {
   }
 
   template <bool WHOLE, bool kOnce>
-  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyWalk& w,
+  __device__ __forceinline__ void issue(const WalkArgs& args, const int (&page)[2], const KeyRange& range,
                                         int key0, int kv_head, uint32_t stage) const {
     int64_t block[2];
 #pragma unroll
@@ -312,12 +299,11 @@ struct Fp8Block {
       block[p] = (int64_t)page[p] * args.h_kv + kv_head;
       const char* kp = args.k_pool + block[p] * (kPageSize * D);
       const char* vp = args.v_pool + block[p] * (kPageSize * D);
-      const PageRead pr(w, key0 + p * kPageSize);
 #pragma unroll
       for (int j = 0; j < kPerPage; ++j) {
         uint32_t ko = k_off[j], vo = v_off[j];
         if (!WHOLE) {
-          const int r = j * kRowsPerInstr + r_in, slot = pr.slot(r);
+          const int r = j * kRowsPerInstr + r_in, slot = range.key(key0 + p * kPageSize + r) & 15;
           ko = slot * D + swz8<D>(r, pos) * 16;
           vo = slot * D + vswz(r, pos) * 16;
         }
@@ -412,7 +398,7 @@ struct BlockPages {
   // blocks b, b + kWaves, ... of the walk
   __device__ __forceinline__ void load(const int32_t* table, const KeyWalk& w, int b, int lane) {
     const int at = min(b + (lane >> 1) * kWaves, w.n - 1);
-    ids = table[PageRead(w, w.tile(at) * 32 + (lane & 1) * kPageSize).page_index];
+    ids = table[KeyRange(w, w.first_tokens(at)).page_index(w.tile(at) * 32 + (lane & 1) * kPageSize)];
   }
   __device__ __forceinline__ void get(int i, int (&page)[2]) const {
     page[0] = __builtin_amdgcn_readlane(ids, 2 * i);
@@ -456,7 +442,8 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
   const int rr = valid ? col : n_rows - 1;
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
-  rb.mask.set(sd.prefix_len + tok, args.window);
+  rb.mask.position = sd.prefix_len + tok;
+  rb.mask.window = args.window;
   Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
   Block block;
   block.init(lane);
@@ -469,12 +456,13 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
       pages.load(args.page_table + sd.pt_off, walk, b_first + i * kWaves, lane);
     int page[2];
     pages.get(i & 31, page);
-    const int key0 = walk.tile(b_first + i * kWaves) * 32;
+    const int b = b_first + i * kWaves, key0 = walk.tile(b) * 32;
+    const KeyRange range(walk, walk.first_tokens(b));
     const uint32_t to = ring_lds + st * Block::kBytes;
     if (i < n_full)
-      block.template issue<true, true>(args, page, walk, key0, kv_head, to);
+      block.template issue<true, true>(args, page, range, key0, kv_head, to);
     else
-      block.template issue<false, true>(args, page, walk, key0, kv_head, to);
+      block.template issue<false, true>(args, page, range, key0, kv_head, to);
   };
   int st_issue = 0, st = 0;
   auto next = [](int x) { return x + 1 == STAGES ? 0 : x + 1; };
@@ -491,11 +479,13 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
       wait_vmcnt<0>();
     }
     const char* stage = ring + st * Block::kBytes;
-    const int key0 = walk.tile(b_first + i * kWaves) * 32;
-    if (i < n_full)
+    const int b = b_first + i * kWaves, key0 = walk.tile(b) * 32;
+    if (i < n_full) {
       block.template step<false>(rb, stage, key0);
-    else
+    } else {
+      rb.mask.visit(walk.first_tokens(b));
       block.template step<true>(rb, stage, key0);
+    }
     st = next(st);
     // every LDS read of the stage has returned before a load refills it
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -557,19 +547,23 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
 
 // ---------------------------------------------------------------- row-split, bf16 cache
 
-// The 64-key tiles of a walk, for run_tiles().
+// The 64-key visits of a walk, for run_tiles(): a tile's number, or its complement where it is visited
+// for first tokens.
 struct WalkKeys {
   KeyWalk w;
-  __device__ __forceinline__ int tile(int i) const { return w.tile(i); }
-  __device__ __forceinline__ bool whole(int t) const {
-    return (t * 64 >= w.lo && (t + 1) * 64 <= w.end) || (t + 1) * 64 <= w.first;
+  __device__ __forceinline__ int tile(int i) const {
+    const int t = w.tile(i);
+    return w.first_tokens(i) ? ~t : t;
   }
-  __device__ __forceinline__ int page_index(int t, int row) const {
-    return PageRead(w, t * 64 + (row & ~(kPageSize - 1))).page_index;
+  __device__ __forceinline__ int key0(int v) const { return (v < 0 ? ~v : v) * 64; }
+  __device__ __forceinline__ bool whole(int v) const { return KeyRange(w, v < 0).whole(key0(v), 64); }
+  __device__ __forceinline__ int page_index(int v, int row) const {
+    return KeyRange(w, v < 0).page_index(key0(v) + (row & ~(kPageSize - 1)));
   }
-  __device__ __forceinline__ int slot(int t, int row) const {
-    return PageRead(w, t * 64 + (row & ~(kPageSize - 1))).slot(row & (kPageSize - 1));
+  __device__ __forceinline__ int slot(int v, int row) const {
+    return KeyRange(w, v < 0).key(key0(v) + row) & (kPageSize - 1);
   }
+  __device__ __forceinline__ void show(WindowMask& mask, int v) const { mask.visit(v < 0); }
 };
 
 // ---------------------------------------------------------------- row-split, 8-bit cache
@@ -731,14 +725,15 @@ struct Fp8Convert {
     in_off = R::kV + row * D + at * 4;
     out_off = R::kV16 + row * (D * 2) + Swz<D>::v(row, at / 2) * 16;
   }
-  template <class Keys>
+  // WHOLE: all keys of the tile are read.
+  template <bool WHOLE, class Keys>
   __device__ __forceinline__ void read(const char* lds, int stage, int tile, const Keys& keys) {
     const char* in = lds + stage * R::kTile + in_off;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       const int r = row + p * kPieceRows;
       const char* s = lds + R::kS + stage * R::kScales + (r >> 4) * R::kScaleStride + kPageSize;
-      scale[p] = __builtin_bit_cast(float, (uint32_t)(uint8_t)s[keys.slot(tile, r)] << 23);
+      scale[p] = __builtin_bit_cast(float, (uint32_t)(uint8_t)s[WHOLE ? r & 15 : keys.slot(tile, r)] << 23);
       if constexpr (kPieceWords == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(in + p * kPieceRows * D);
         raw[4 * p] = x.x; raw[4 * p + 1] = x.y; raw[4 * p + 2] = x.z; raw[4 * p + 3] = x.w;
@@ -804,7 +799,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
   forget(s1);
   ring_barrier<2 * R::kLoads>();  // tile kt_a has landed, for everyone
   auto convert_all = [&](auto w) { cv.template convert<decltype(w)::value>(lds, 0); };
-  cv.read(lds, 0, keys.tile(kt_a), keys);
+  cv.template read<false>(lds, 0, keys.tile(kt_a), keys);
   static_for<Fp8Convert<D, NW>::kWords>(convert_all);
   rb.template qk<2, R::kScaleStride>(k_stage(0), scales(0), lane, s0);
   if (kt_u > kt_a) {
@@ -823,7 +818,9 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
         auto at_slot = [&](auto slot) {
           constexpr int i = decltype(slot)::value;
           constexpr int kFirst = 6, kStep = D == 128 ? 2 : 1;
-          if constexpr (i == 1) cv.read(lds, s_next, keys.tile(cur + 1), keys);
+          // (up to a round's last iteration the next tile has the round's form)
+          if constexpr (i == 1)
+            cv.template read<!kMask && s_next != 0>(lds, s_next, keys.tile(cur + 1), keys);
           if constexpr (i == Rows::kLoadSlot) {
             asm volatile("" : "+s"(page_next));  // the page id is first needed here, not before
             issue(cur + 3, (s + 3) % kRound);
@@ -834,10 +831,11 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
         };
         const typename Rows::KSide next(rb, k_stage(s_next), scales(s_next));
         const char* v_cur = lds + (s & 1) * (2 * R::kTile);  // + the bias in rb.v_off
+        if constexpr (kMask) keys.show(rb.mask, keys.tile(cur));
         if constexpr (s & 1)
-          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s1, s0, keys.tile(cur) * 64, half, at_slot);
+          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s1, s0, keys.key0(keys.tile(cur)), half, at_slot);
         else
-          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s0, s1, keys.tile(cur) * 64, half, at_slot);
+          rb.template fused<kMask, true, kSpeculate>(next, v_cur, s0, s1, keys.key0(keys.tile(cur)), half, at_slot);
         // (the scalar load goes here: see run_tiles)
         __builtin_amdgcn_sched_barrier(0);
         next_page(cur + 4);
@@ -858,10 +856,13 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
     constexpr bool kMask = decltype(mask)::value;
     const typename Rows::KSide none(rb, nullptr, nullptr);
     const char* v_last = lds + ((last - kt_a) & 1) * (2 * R::kTile);
+    if constexpr (kMask) keys.show(rb.mask, keys.tile(last));
     if ((last - kt_a) & 1)
-      rb.template fused<kMask, false, false>(none, v_last, s1, s0, keys.tile(last) * 64, half, [](auto) {});
+      rb.template fused<kMask, false, false>(none, v_last, s1, s0, keys.key0(keys.tile(last)), half,
+                                                   [](auto) {});
     else
-      rb.template fused<kMask, false, false>(none, v_last, s0, s1, keys.tile(last) * 64, half, [](auto) {});
+      rb.template fused<kMask, false, false>(none, v_last, s0, s1, keys.key0(keys.tile(last)), half,
+                                                   [](auto) {});
   };
   if (kt_u == kt_b)
     final_tile(std::false_type{});
@@ -903,7 +904,8 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int rr = valid ? r : (n_rows - 1);
   const int tok = rr / gqa;
   const int hq = kv_head * gqa + rr % gqa;
-  rb.mask.set(sd.prefix_len + tok, args.window);
+  rb.mask.position = sd.prefix_len + tok;
+  rb.mask.window = args.window;
   using Block = std::conditional_t<kFp8, Fp8Block<D>, Bf16Block<D>>;
   Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
 
