@@ -574,14 +574,17 @@ __device__ __forceinline__ void ring_barrier_written() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// The workgroup's LDS: 4 stages each of K and V tiles as they come, D bytes a row, their scale bytes,
-// and two V tiles in bf16.
-template <int D, int NW>
+// The workgroup's LDS: stages of K and V tiles as they come, D bytes a row, of scale bytes, and two V
+// tiles in bf16.  The long ring has 4 stages of each; the short one 3, and 2 for V, whose loads then
+// stay a tile behind: at head dim 128 two workgroups of 4 wavefronts fit a compute unit.
+template <int D, int NW, bool SHORT>
 struct Fp8Ring {
-  static constexpr int kStages = 4;
+  static constexpr int kStages = SHORT ? 3 : 4, kVStages = SHORT ? 2 : 4;
+  static constexpr int kLag = SHORT ? 1 : 0, kRound = SHORT ? 6 : 4;
   static constexpr int kTile = 64 * D;  // K (or V) tile
   static constexpr int kScales = NW * 256;  // a wavefront's 64 lanes' worth
-  static constexpr int kV = kStages * kTile, kS = 2 * kV, kV16 = kS + kStages * kScales;
+  static constexpr int kV = kStages * kTile, kS = kV + kVStages * kTile;
+  static constexpr int kV16 = kS + kStages * kScales;
   static constexpr int kBytes = kV16 + 2 * (2 * kTile);
   static constexpr int kLdsBytes = kBytes > NW * 32 * D * 4 ? kBytes : NW * 32 * D * 4;  // (write_rows)
   // a tile's load instructions, 1 KiB each: every wavefront takes as many of K as of V, or, where
@@ -589,7 +592,12 @@ struct Fp8Ring {
   static constexpr int kInstr = kTile / 1024, kRowsPerInstr = 1024 / D;
   static constexpr bool kBoth = kInstr >= NW;
   static constexpr int kPerWave = kBoth ? kInstr / NW : 1;
-  static constexpr int kLoads = (kBoth ? 2 * kPerWave : 1) + 1;
+  static constexpr int kTileLoads = (kBoth ? 2 * kPerWave : 1) + 1;  // of K, V and scale bytes
+  static_assert(kBoth || !SHORT, "V loads of their own");
+  // loads of an iteration that its successor's barrier leaves in flight, and those of the prologue
+  // behind the first tile's
+  static constexpr int kYoungest = SHORT ? kPerWave + 1 : kTileLoads;
+  static constexpr int kBehindFirst = kYoungest + kTileLoads;
   // the scale bytes of page p of a tile are where its first wavefront put them
   static constexpr int kScaleStride = kBoth ? NW / 4 * 256 : 256;
   // V rows a wavefront turns into bf16, and its lanes' bytes of them
@@ -597,10 +605,10 @@ struct Fp8Ring {
 };
 
 // Rows of one wavefront with what the tile walk needs of them.
-template <int D, int NW>
+template <int D, int NW, bool SHORT>
 struct TileRows8 : Rows8<D> {
   using Base = Rows8<D>;
-  using R = Fp8Ring<D, NW>;
+  using R = Fp8Ring<D, NW, SHORT>;
   int k8_off[2 * Base::kParts];  // this lane's 16-byte pieces of key row `col`, within a K tile
   int ks_off;                    // its scale byte within a stage's
   int wave_page, k_pos, lane;
@@ -653,9 +661,9 @@ struct TileRows8 : Rows8<D> {
 };
 
 // This wavefront's share of a tile's loads.
-template <int D, int NW>
+template <int D, int NW, bool SHORT>
 struct Fp8Loader {
-  using R = Fp8Ring<D, NW>;
+  using R = Fp8Ring<D, NW, SHORT>;
   uint32_t k_off[R::kPerWave], v_off[R::kPerWave];  // within the (page, KV head) block
   int row0, r_in, pos;
   bool values;  // !kBoth: this wavefront loads V
@@ -672,21 +680,22 @@ struct Fp8Loader {
       v_off[j] = (row & 15) * D + pos * 16;
     }
   }
-  // `stage`: of the ring, with the wavefront's place among the scale bytes.
-  template <class Keys>
+  // Loads K rows and scale bytes (K), V rows (V) of a tile into stages of the ring.
+  template <bool K, bool V, class Keys>
   __device__ __forceinline__ void issue(const WalkArgs& args, int page, int tile, const Keys& keys,
-                                        int kv_head, uint32_t ring, int stage, int wave, int lane) const {
+                                        int kv_head, uint32_t ring, int k_stage, int v_stage, int wave,
+                                        int lane) const {
     const int64_t block = (int64_t)page * args.h_kv + kv_head;
     const char* kp = args.k_pool + block * (kPageSize * D);
     const char* vp = args.v_pool + block * (kPageSize * D);
-    const uint32_t to = ring + stage * R::kTile;
+    const uint32_t k_to = ring + k_stage * R::kTile, v_to = ring + R::kV + v_stage * R::kTile;
     auto load = [&](uint32_t ko, uint32_t vo, int j) {
-      const uint32_t at = to + (row0 + j * R::kRowsPerInstr) * D;
+      const uint32_t at = (row0 + j * R::kRowsPerInstr) * D;
       if constexpr (R::kBoth) {
-        async_load16<false>(kp, ko, at);
-        async_load16<false>(vp, vo, at + R::kV);
+        if (K) async_load16<false>(kp, ko, k_to + at);
+        if (V) async_load16<false>(vp, vo, v_to + at);
       } else {
-        async_load16<false>(values ? vp : kp, values ? vo : ko, values ? at + R::kV : at);
+        async_load16<false>(values ? vp : kp, values ? vo : ko, (values ? v_to : k_to) + at);
       }
     };
     if (keys.whole(tile)) {
@@ -700,15 +709,16 @@ struct Fp8Loader {
         load(slot * D + swz8<D>(row, pos) * 16, slot * D + pos * 16, j);
       }
     }
-    async_load4(args.scale + block * kScaleBytesPerPage, (lane & 7) * 4,
-                ring + R::kS + stage * R::kScales + wave * 256);
+    if (K)
+      async_load4(args.scale + block * kScaleBytesPerPage, (lane & 7) * 4,
+                  ring + R::kS + k_stage * R::kScales + wave * 256);
   }
 };
 
 // The wavefront's V rows of a tile, from 8 bits to bf16 where the transposing reads expect them.
-template <int D, int NW>
+template <int D, int NW, bool SHORT>
 struct Fp8Convert {
-  using R = Fp8Ring<D, NW>;
+  using R = Fp8Ring<D, NW, SHORT>;
   static constexpr int kWords = R::kLaneBytes / 4;
   static constexpr int kPieces = kWords > 4 ? kWords / 4 : 1;  // of 16 bytes (or one of 8)
   static constexpr int kPieceRows = kWords > 4 ? R::kRowsPerWave / kPieces : R::kRowsPerWave;
@@ -727,12 +737,13 @@ struct Fp8Convert {
   }
   // WHOLE: all keys of the tile are read.
   template <bool WHOLE, class Keys>
-  __device__ __forceinline__ void read(const char* lds, int stage, int tile, const Keys& keys) {
-    const char* in = lds + stage * R::kTile + in_off;
+  __device__ __forceinline__ void read(const char* lds, int s_stage, int v_stage, int tile,
+                                       const Keys& keys) {
+    const char* in = lds + v_stage * R::kTile + in_off;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       const int r = row + p * kPieceRows;
-      const char* s = lds + R::kS + stage * R::kScales + (r >> 4) * R::kScaleStride + kPageSize;
+      const char* s = lds + R::kS + s_stage * R::kScales + (r >> 4) * R::kScaleStride + kPageSize;
       scale[p] = __builtin_bit_cast(float, (uint32_t)(uint8_t)s[WHOLE ? r & 15 : keys.slot(tile, r)] << 23);
       if constexpr (kPieceWords == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(in + p * kPieceRows * D);
@@ -760,47 +771,63 @@ struct Fp8Convert {
 // Walks tiles [kt_a, kt_b) of a walk, those below kt_mid without a mask: run_tiles() over the 8-bit
 // cache.  At the barrier that opens iteration cur, K tile cur+1 and V tile cur+1 have landed as they
 // are and V tile cur is there in bf16; in the iteration every wavefront turns its rows of V tile cur+1
-// into bf16, beside the softmax of tile cur, and issues tile cur+3.
-template <int D, int NW, class Keys>
-__device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs& args, ConstI32Ptr pt,
-                                           int kt_a, int kt_mid, int kt_b, const Keys& keys,
-                                           int kv_head, char* lds, int wave, int lane) {
-  using R = Fp8Ring<D, NW>;
-  using Rows = TileRows8<D, NW>;
-  constexpr int kRound = R::kStages;
+// into bf16, beside the softmax of tile cur, and issues K tile cur+3 and V tile cur+3 (cur+2 with the
+// short ring).
+template <int D, int NW, bool SHORT, class Keys>
+__device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const WalkArgs& args,
+                                           ConstI32Ptr pt, int kt_a, int kt_mid, int kt_b,
+                                           const Keys& keys, int kv_head, char* lds, int wave,
+                                           int lane) {
+  using R = Fp8Ring<D, NW, SHORT>;
+  using Rows = TileRows8<D, NW, SHORT>;
+  using Convert = Fp8Convert<D, NW, SHORT>;
+  constexpr int kRound = R::kRound;
   static_assert(kWarmTiles % kRound == 0, "the walk's head is a whole number of ring rounds");
   if (kt_a >= kt_b) return;
   const int half = lane >> 5;
   const int last = kt_b - 1;
   const int kt_u = kt_mid >= kt_b ? kt_b : kt_a + (kt_mid - kt_a) / kRound * kRound;
   const uint32_t ring = lds_address(lds);
-  Fp8Loader<D, NW> ld;
+  Fp8Loader<D, NW, SHORT> ld;
   ld.init(wave, lane);
-  Fp8Convert<D, NW> cv;
+  Convert cv;
   cv.init(wave, lane);
-  int page_next = 0;
+  int page_next = 0, page_1 = 0;  // ids of the next tile's page, and of the one before it
   auto next_page = [&](int i) {
+    if (SHORT) page_1 = page_next;
     const int t = keys.tile(min(i, last));
     page_next = pt[__builtin_amdgcn_readfirstlane(keys.page_index(t, ld.row0))];
   };
-  auto issue = [&](int i, int stage) {
-    ld.issue(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring, stage, wave, lane);
+  // K tile i, and V tile i - kLag if v_stage is one (with the short ring first: the wait for it leaves K
+  // in flight)
+  auto issue = [&](int i, int k_stage, int v_stage) {
+    if constexpr (SHORT) {
+      if (v_stage >= 0)
+        ld.template issue<false, true>(args, page_1, keys.tile(min(i - 1, last)), keys, kv_head, ring, 0,
+                                       v_stage, wave, lane);
+      ld.template issue<true, false>(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring,
+                                     k_stage, 0, wave, lane);
+    } else {
+      ld.template issue<true, true>(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring, k_stage,
+                                    v_stage, wave, lane);
+    }
   };
   auto k_stage = [&](int s) { return lds + s * R::kTile; };
   auto scales = [&](int s) { return lds + R::kS + s * R::kScales; };
+  // prologue: K tiles kt_a .. kt_a+2 and V tiles up to kt_a+2-kLag
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     next_page(kt_a + i);
-    issue(kt_a + i, i);
+    issue(kt_a + i, i, i - R::kLag);
   }
   next_page(kt_a + 3);
   f32x16 s0[2], s1[2];
   forget(s0);
   forget(s1);
-  ring_barrier<2 * R::kLoads>();  // tile kt_a has landed, for everyone
+  ring_barrier<R::kBehindFirst>();  // tile kt_a has landed, for everyone
   auto convert_all = [&](auto w) { cv.template convert<decltype(w)::value>(lds, 0); };
-  cv.template read<false>(lds, 0, keys.tile(kt_a), keys);
-  static_for<Fp8Convert<D, NW>::kWords>(convert_all);
+  cv.template read<false>(lds, 0, 0, keys.tile(kt_a), keys);
+  static_for<Convert::kWords>(convert_all);
   rb.template qk<2, R::kScaleStride>(k_stage(0), scales(0), lane, s0);
   if (kt_u > kt_a) {
     float mx = -INFINITY;
@@ -811,25 +838,26 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
   auto round = [&](int kt, auto mask, auto spec) {
     constexpr bool kMask = decltype(mask)::value, kSpeculate = decltype(spec)::value;
     auto iteration = [&](auto s_const) {
-      constexpr int s = decltype(s_const)::value, s_next = (s + 1) % kRound;
+      constexpr int s = decltype(s_const)::value;
+      constexpr int k_next = (s + 1) % R::kStages, v_next = (s + 1) % R::kVStages;
       const int cur = kt + s;
       if (cur < last) {
-        ring_barrier_written<R::kLoads>();
+        ring_barrier_written<R::kYoungest>();
         auto at_slot = [&](auto slot) {
           constexpr int i = decltype(slot)::value;
           constexpr int kFirst = 6, kStep = D == 128 ? 2 : 1;
           // (up to a round's last iteration the next tile has the round's form)
           if constexpr (i == 1)
-            cv.template read<!kMask && s_next != 0>(lds, s_next, keys.tile(cur + 1), keys);
+            cv.template read<!kMask && s + 1 < kRound>(lds, k_next, v_next, keys.tile(cur + 1), keys);
           if constexpr (i == Rows::kLoadSlot) {
             asm volatile("" : "+s"(page_next));  // the page id is first needed here, not before
-            issue(cur + 3, (s + 3) % kRound);
+            issue(cur + 3, (s + 3) % R::kStages, (s + 3 - R::kLag) % R::kVStages);
           }
           if constexpr (i >= kFirst && (i - kFirst) % kStep == 0 &&
-                        (i - kFirst) / kStep < Fp8Convert<D, NW>::kWords)
-            cv.template convert<(i - kFirst) / kStep>(lds, s_next & 1);
+                        (i - kFirst) / kStep < Convert::kWords)
+            cv.template convert<(i - kFirst) / kStep>(lds, (s + 1) & 1);
         };
-        const typename Rows::KSide next(rb, k_stage(s_next), scales(s_next));
+        const typename Rows::KSide next(rb, k_stage(k_next), scales(k_next));
         const char* v_cur = lds + (s & 1) * (2 * R::kTile);  // + the bias in rb.v_off
         if constexpr (kMask) keys.show(rb.mask, keys.tile(cur));
         if constexpr (s & 1)
@@ -851,7 +879,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
   for (; __builtin_expect_with_probability(kt < end_u, 1, 0.995); kt += kRound)
     round(kt, std::false_type{}, std::true_type{});
   for (; kt < last; kt += kRound) round(kt, std::true_type{}, std::false_type{});
-  ring_barrier_written<R::kLoads>();  // the last V tile is there in bf16, for everyone
+  ring_barrier_written<R::kYoungest>();  // the last V tile is there in bf16, for everyone
   auto final_tile = [&](auto mask) {
     constexpr bool kMask = decltype(mask)::value;
     const typename Rows::KSide none(rb, nullptr, nullptr);
@@ -873,13 +901,13 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW>& rb, const WalkArgs&
 
 // Chunks: a workgroup of NW wavefronts owns NW * 32 query rows of one KV head and walks 64-key tiles,
 // as prefill_kernel does, along the tiles of its rows' windows.
-// NV: stages of the V ring, or 0 for the 8-bit cache.
-template <int D, int NW, int NV>
+// SHORT: with the short ring, two workgroups to a compute unit.
+template <int D, int NW, bool kFp8, bool SHORT = false>
 __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
-  constexpr bool kFp8 = NV == 0;
-  using Shape = PrefillShape<D, NW, kFp8 ? 4 : NV>;
-  using Rows = std::conditional_t<kFp8, TileRows8<D, NW>, RowBlock<D, WindowMask>>;
-  constexpr int kLdsBytes = kFp8 ? Fp8Ring<D, NW>::kLdsBytes : Shape::kLdsBytes;
+  constexpr int NV = SHORT ? 2 : 4;
+  using Shape = PrefillShape<D, NW, NV>;
+  using Rows = std::conditional_t<kFp8, TileRows8<D, NW, SHORT>, RowBlock<D, WindowMask>>;
+  constexpr int kLdsBytes = kFp8 ? Fp8Ring<D, NW, SHORT>::kLdsBytes : Shape::kLdsBytes;
   __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes];
 
   const SeqDesc* descs = args.inline_descs;
@@ -917,7 +945,7 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int kt_mid = max(kt_begin, min(kt_end, keys.w.n_full));
   ConstI32Ptr pt = (ConstI32Ptr)(args.page_table + sd.pt_off);
   if constexpr (kFp8) {
-    run_tiles8<D, NW>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, lds, wave, lane);
+    run_tiles8<D, NW, SHORT>(rb, args, pt, kt_begin, kt_mid, kt_end, keys, kv_head, lds, wave, lane);
   } else {
     const Ring stages{lds, lds_address(lds)};
     TileLoader<D, NW> loader;

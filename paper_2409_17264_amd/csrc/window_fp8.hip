@@ -102,19 +102,14 @@ hipError_t launch_keys(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStr
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool kFp8>
 hipError_t launch_rows(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStream_t stream) {
-  if (a.scale != nullptr) {
-    if (lp.q_blocks == 2)
-      hipLaunchKernelGGL((row_walk_kernel<D, 8, 0>), dim3(grid), dim3(512), 0, stream, a);
-    else
-      hipLaunchKernelGGL((row_walk_kernel<D, 4, 0>), dim3(grid), dim3(256), 0, stream, a);
-  } else if (lp.q_blocks == 2)
-    hipLaunchKernelGGL((row_walk_kernel<D, 8, 4>), dim3(grid), dim3(512), 0, stream, a);
+  if (lp.q_blocks == 2)
+    hipLaunchKernelGGL((row_walk_kernel<D, 8, kFp8>), dim3(grid), dim3(512), 0, stream, a);
   else if (lp.paired)
-    hipLaunchKernelGGL((row_walk_kernel<128, 4, 2>), dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((row_walk_kernel<128, 4, kFp8, true>), dim3(grid), dim3(256), 0, stream, a);
   else
-    hipLaunchKernelGGL((row_walk_kernel<D, 4, 4>), dim3(grid), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((row_walk_kernel<D, 4, kFp8>), dim3(grid), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -153,8 +148,9 @@ hipError_t launch_walks(const LaunchPlan& lp, WalkArgs& a, hipStream_t stream) {
       max_split = std::max(max_split, sd.n_split);
     }
     if (slot1 == slot0) continue;
-    hipError_t e = lp.key_split ? launch_keys<D>(lp, a, slot1 - slot0, stream)
-                                : launch_rows<D>(lp, a, slot1 - slot0, stream);
+    hipError_t e = lp.key_split         ? launch_keys<D>(lp, a, slot1 - slot0, stream)
+                   : a.scale != nullptr ? launch_rows<D, true>(lp, a, slot1 - slot0, stream)
+                                        : launch_rows<D, false>(lp, a, slot1 - slot0, stream);
     if (e != hipSuccess) return e;
     if (max_split == 1) continue;
     MergeArgs m{};

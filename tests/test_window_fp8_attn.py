@@ -129,6 +129,18 @@ def test_long_walks(heads, fp8, prefix, chunk, window, sinks):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("fp8, prefix, chunk, window", [
+    (True, 6000, 200, None), (True, 9000, 130, None), (True, 9007, 130, 8000), (False, 9007, 130, 8000),
+    (False, 6011, 200, 6000)])
+def test_workgroups_in_pairs(fp8, prefix, chunk, window):
+    """Launches that take two 128-row workgroups to a compute unit, with the short ring."""
+    e, grid, _, _ = medha.describe_plan([prefix], [chunk], 32, 8, 128, 256)
+    assert e[0].mode == 0 and e[0].rows_per_wg == 128 and grid > 256
+    c = Case(32, 8, 128, [prefix], [chunk], window, 5, fp8, seed=chunk)
+    c.check(*c.run())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("k_std", [6.0, 0.0])
 @pytest.mark.parametrize("fp8, window", [(False, 3000), (True, 3000), (True, None)])
 def test_peaked_and_flat_rows(fp8, window, k_std):
