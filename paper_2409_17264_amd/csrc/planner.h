@@ -97,6 +97,11 @@ inline WalkCost walk_cost(int head_dim, int q_blocks) {
 // measured 1.02) and a twelfth more at 128 (a pair 1.11, measured 1.05): where walks are long, a
 // small form wins by the whole round that it saves or not at all.
 constexpr WalkCost kAloneCost[2] = {{0.65, 9.0, 1}, {1.25, 8.0, 1}}, kPairedCost{1.85, 8.0, 2};
+// In pairs over the 8-bit cache, where both read half as much: a pair of long walks takes 1.04 to 1.07
+// of the large form's time (1500 tokens at 65536, 32/8 heads, 1479 us large, 1543 in pairs; 1000 at
+// 131072 1874 and 1997), and wins where 128 rows fit better (111 at 524291, 16/2 heads, 493 -> 465,
+// 8/1 257 -> 246).
+constexpr WalkCost kPairedCostFp8{1.75, 8.0, 2};
 
 constexpr int64_t kShortPairedTiles = 10;
 
@@ -243,7 +248,10 @@ inline LaunchWalks launch_walks(const LaunchPlan& lp, int h_kv, int gqa) {
     lw.dealt.push_back(uneven);
     for (int64_t c = classes; c-- > 0;) {
       const int64_t lo = c * n_rt / classes, hi = (c + 1) * n_rt / classes;
-      const int64_t t = tiles_at(sd, lp.shape, gqa, uneven ? (lo + hi) / 2 : n_rt - 1);
+      // (behind a window walks differ by a tile with the place of the window's edges in theirs)
+      const int64_t t = !uneven && sd.kv_len > lp.shape.window.keys
+                            ? kv_tiles_of(sd, lp.shape)
+                            : tiles_at(sd, lp.shape, gqa, uneven ? (lo + hi) / 2 : n_rt - 1);
       lw.classes.push_back(WalkClass{t, hi - lo});
       lw.total_tiles += t * (hi - lo) * h_kv;
       if (t > 0) lw.busy += (hi - lo) * h_kv;
@@ -486,12 +494,13 @@ inline int64_t simple_steps(LaunchPlan& lp, int h_kv, int gqa, int target_wgs) {
 // if its partials fit it (so that every workspace of the reported size gives the same plan, whatever
 // the choices on the way to it look at), and otherwise takes the KV ranges that are expected to be
 // fastest among those whose partials do; the simple rule's need (`min_bytes`) is the least a call has
-// to bring.  `window`: of the rows.
+// to bring.  `window`: of the rows; `fp8`: the cache has 8 bits.
 inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int head_dim,
-                      int num_cus, size_t budget = SIZE_MAX, const Window& window = {}) {
+                      int num_cus, size_t budget = SIZE_MAX, const Window& window = {},
+                      bool fp8 = false) {
   Plan plan;
   if (budget != SIZE_MAX) {
-    plan = make_plan(seqs, batch, h_q, h_kv, head_dim, num_cus, SIZE_MAX, window);
+    plan = make_plan(seqs, batch, h_q, h_kv, head_dim, num_cus, SIZE_MAX, window, fp8);
     if (plan.part_rows == 0 || plan.bytes <= budget) return plan;
     plan = Plan{};
   }
@@ -628,10 +637,11 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
       // 8/2, 27.9 -> 29.7); a stream of one row tile alone wants the long ring (16 tokens at 1M 114
       // us, 127 in pairs).
       if (head_dim == 128 && behind && shared) {
+        const WalkCost& cost = fp8 ? kPairedCostFp8 : kPairedCost;
         if (big)
-          try_small(kPairedCost, true, 0.98, num_cus + 1, INT64_MAX, kShortPairedTiles, 0.90);
+          try_small(cost, true, 0.98, num_cus + 1, INT64_MAX, kShortPairedTiles, 0.90);
         else
-          try_small(kPairedCost, true, 0.83, num_cus + 1, INT64_MAX);
+          try_small(cost, true, 0.83, num_cus + 1, INT64_MAX);
       }
     }
   }

@@ -178,17 +178,17 @@ bool window_of(int32_t keys, int32_t sinks, bool optional, Window& w) {
 }
 
 Plan walk_plan(const std::vector<SeqInput>& seqs, int h_q, int h_kv, int d, size_t budget,
-               const Window& w) {
-  return make_plan(seqs.data(), (int)seqs.size(), h_q, h_kv, d, current_num_cus(), budget, w);
+               const Window& w, bool fp8) {
+  return make_plan(seqs.data(), (int)seqs.size(), h_q, h_kv, d, current_num_cus(), budget, w, fp8);
 }
 
 size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32_t batch,
                       int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, int32_t window,
-                      int32_t sinks, bool optional) {
+                      int32_t sinks, bool fp8) {
   Window w;
   if (batch < 0 || (batch > 0 && (prefix_len == nullptr || chunk_len == nullptr))) return 0;
   if (check_heads(num_q_heads, num_kv_heads, head_dim, kPageSize) != MEDHA_OK) return 0;
-  if (!window_of(window, sinks, optional, w)) return 0;
+  if (!window_of(window, sinks, fp8, w)) return 0;
   std::vector<SeqInput> seqs(batch);
   int64_t row = 0;
   for (int b = 0; b < batch; ++b) {
@@ -198,7 +198,8 @@ size_t walk_workspace(const int32_t* prefix_len, const int32_t* chunk_len, int32
     row += chunk_len[b];
     if (row > INT32_MAX) return 0;
   }
-  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w).workspace_bytes();
+  return walk_plan(seqs, num_q_heads, num_kv_heads, head_dim, SIZE_MAX, w, fp8)
+      .workspace_bytes();
 }
 
 // A call on either cache.  `kv` describes its pools, `scale` is null for the bf16 one; `alloc`: asked
@@ -236,7 +237,8 @@ int walk_attn(const void* q, const medha_kv_cache* kv, const void* scale, const 
     if (row > INT32_MAX) return MEDHA_ERR_INVALID_ARG;
   }
   const Plan plan = walk_plan(seqs, num_q_heads, kv->num_kv_heads, kv->head_dim,
-                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window);
+                              alloc ? SIZE_MAX : usable_bytes(workspace, workspace_bytes), window,
+                              scale != nullptr);
   if (alloc) {
     workspace_bytes = plan.workspace_bytes();
     workspace = alloc(workspace_bytes, context);
