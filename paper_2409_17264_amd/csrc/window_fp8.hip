@@ -29,8 +29,7 @@ int check_cache(const medha_kv_cache_fp8* kv) {
 }
 
 // Both directions: tokens [first[b], first[b] + count[b]) of every sequence, `least` of them or more.
-template <class Kernel>
-int move_tokens(Kernel kernel, const void* k_rows, const void* v_rows, const medha_kv_cache_fp8* kv,
+int move_tokens(bool append, const void* k_rows, const void* v_rows, const medha_kv_cache_fp8* kv,
                 const int32_t* page_table, const int64_t* page_table_offs, const int32_t* first,
                 const int32_t* count, int32_t batch, int32_t least, void* hip_stream) {
   const int rc = check_cache(kv);
@@ -54,18 +53,23 @@ int move_tokens(Kernel kernel, const void* k_rows, const void* v_rows, const med
     rows += count[b];
     if (rows > INT32_MAX) return MEDHA_ERR_INVALID_ARG;
   }
+  // K and V rows in bf16 (see kv_read_fp8_kernel)
+  const bool once = rows * kv->num_kv_heads * kv->head_dim * 4 >= kLastLevelCacheBytes;
+  const auto kernel = append ? kv_append_fp8_kernel
+                      : once ? kv_read_fp8_kernel<true>
+                             : kv_read_fp8_kernel<false>;
   // validated in full before the first launch; up to kMaxInlineSeq sequences per launch
   int64_t src_row = 0;
   for (int b0 = 0; b0 < batch; b0 += kMaxInlineSeq) {
     Fp8CacheArgs a{};
     a.k_rows = static_cast<uint4*>(const_cast<void*>(k_rows));
     a.v_rows = static_cast<uint4*>(const_cast<void*>(v_rows));
-    a.k_pool = static_cast<uint2*>(const_cast<void*>(kv->k_pool));
-    a.v_pool = static_cast<uint2*>(const_cast<void*>(kv->v_pool));
+    a.k_pool = const_cast<void*>(kv->k_pool);
+    a.v_pool = const_cast<void*>(kv->v_pool);
     a.scale = static_cast<uint8_t*>(const_cast<void*>(kv->scale));
     a.page_table = page_table;
     a.h_kv = kv->num_kv_heads;
-    a.words_per_row = kv->head_dim / 8;
+    a.words_per_row = kv->head_dim / (append ? 16 : 8);
     a.num_pages = kv->num_pages;
     a.n_seq = std::min(kMaxInlineSeq, batch - b0);
     int32_t rank = 0;
@@ -310,14 +314,14 @@ int medha_kv_append_fp8(const void* k_new, const void* v_new, const medha_kv_cac
                         const int32_t* page_table, const int64_t* page_table_offs,
                         const int32_t* prefix_len, const int32_t* chunk_len, int32_t batch,
                         void* hip_stream) {
-  return move_tokens(kv_append_fp8_kernel, k_new, v_new, kv, page_table, page_table_offs, prefix_len,
+  return move_tokens(true, k_new, v_new, kv, page_table, page_table_offs, prefix_len,
                      chunk_len, batch, 1, hip_stream);
 }
 
 int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
                       const int64_t* page_table_offs, const int32_t* first, const int32_t* count,
                       int32_t batch, void* k_out, void* v_out, void* hip_stream) {
-  return move_tokens(kv_read_fp8_kernel, k_out, v_out, kv, page_table, page_table_offs, first, count,
+  return move_tokens(false, k_out, v_out, kv, page_table, page_table_offs, first, count,
                      batch, 0, hip_stream);
 }
 

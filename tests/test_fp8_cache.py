@@ -178,6 +178,23 @@ def ref_bits(x):
 
 
 @pytest.mark.gpu
+def test_a_read_larger_than_the_last_level_cache():
+    """65537 tokens of 8 heads, 268 MB of rows: the way that stores past the caches."""
+    d, h_kv, n = 128, 8, 65537
+    pages = wl.pages_for(n)
+    gen = torch.Generator("cuda").manual_seed(1)
+    pool = torch.randint(0, 127, (2, pages, h_kv, 16, d), generator=gen, device="cuda", dtype=torch.uint8)
+    scale = torch.randint(100, 150, (pages, h_kv, 2, 16), generator=gen, device="cuda", dtype=torch.uint8)
+    table = torch.randperm(pages, generator=gen, device="cuda").to(torch.int32)
+    got = medha.kv_read_fp8(pool[0].view(FP8), pool[1].view(FP8), scale, table, [0, pages], [0], [n])
+    power = (scale.to(torch.int32) << 23).view(torch.float32)
+    for w in (0, 1):
+        rows = pool[w].view(FP8).float() * power[:, :, w, :, None]      # exact
+        want = rows[table.long()].permute(0, 2, 1, 3).reshape(-1, h_kv, d)[:n].to(torch.bfloat16)
+        assert torch.equal(got[w], want)
+
+
+@pytest.mark.gpu
 def test_pages_outside_the_pool_are_skipped_and_read_as_zero():
     d, h_kv = 128, 2
     rng = np.random.default_rng(8)
