@@ -105,6 +105,17 @@ constexpr WalkCost kPairedCostFp8{1.75, 8.0, 2};
 
 constexpr int64_t kShortPairedTiles = 10;
 
+// Key-split launches over the 8-bit cache or behind a window, at head dim 128, whose ranges are chosen
+// like those of a row-split launch: two workgroups to a compute unit, a 128-key tile at 5.8 TB/s for
+// all of them, 6 us of start and end.  Against the rule of so many workgroups a unit (which is kept
+// where the estimate gains less): 16 decodes of 8192 at 32/8 heads over the 8-bit cache 79.7 -> 70.2 us,
+// 16 of 40000 at 8/1 64.0 -> 50.4; 64 behind a window of 1000 57.0 -> 48.2, 60 over the 8-bit cache and
+// a window of 4096 86.4 -> 79.2; 60 of 8192 at 8/1, window 300000, 68.2 -> 71.5.  At head dim 64, where
+// three share a unit, 18 batches take 0.85 to 1.07 of the time, 1.00 in the mean: they keep the rule.
+inline WalkCost keys_cost(bool fp8) { return fp8 ? WalkCost{2.9, 6.0, 2} : WalkCost{5.7, 6.0, 2}; }
+// Launches of less work keep the rule, since an estimate is host time; one launch is estimated.
+constexpr double kPlannedKeysUs = 30.0, kWorthPlannedKeys = 0.92;
+
 // What partials cost: a launch, then their bytes.  The merge kernel takes 8 us for 31 MB and 17
 // to 18 us for 99 MB; the constants ask 10 and 25, since partials are written and held as well.
 constexpr double kMergeLaunchUs = 3.0, kMergeBytesPerUs = 4.5e6;
@@ -554,6 +565,19 @@ inline Plan make_plan(const SeqInput* seqs, int batch, int h_q, int h_kv, int he
     // heads, 87.2 -> 88.9); long walks fill their rounds with 8.
     const int64_t six = simple_steps(plan.keys, h_kv, gqa, num_cus * 6);
     if (six >= 6 && six <= kShortWalkTiles) keys_steps = six;
+    if ((fp8 || window.keys != INT32_MAX) && head_dim == 128 &&
+        (int)plan.keys.descs.size() <= kMaxInlineSeq) {
+      const LaunchWalks walks = launch_walks(plan.keys, h_kv, gqa);
+      const WalkCost cost = keys_cost(fp8);
+      if (even_us(walks, walks.longest, num_cus, cost) > kPlannedKeysUs) {
+        double us;
+        const int64_t steps = choose_steps(plan.keys, walks, h_kv, num_cus, cost, keys_steps, kMinTiles,
+                                           row_bytes, fit - rows_min, us);
+        if (us < kWorthPlannedKeys * launch_us(plan.keys, walks, h_kv, num_cus, cost, keys_steps,
+                                               kMinTiles, row_bytes))
+          keys_steps = steps;
+      }
+    }
     keys_rows = split_size(plan.keys, h_kv, keys_steps, kMinTiles).part_rows;
     // A launch that leaves compute units idle at ranges of 4 tiles, and is merged anyway, takes the
     // shortest ranges that find a unit each: a walk is a chain of trips to HBM, 1.2 us a tile.  (One
