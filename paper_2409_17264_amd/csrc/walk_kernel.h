@@ -406,7 +406,11 @@ struct BlockPages {
   }
 };
 
-// STAGES blocks of every wavefront are in flight while it waits for the first of them.
+// STAGES blocks of every wavefront are in flight while it waits for the first of them.  The loads are
+// non-temporal (see async_stream16), also where sequences share their keys: looking that up in the page
+// table, and a second copy of the walk for it, take 64 decodes that share 8192 keys over the 8-bit cache
+// from 114 to 115 us, behind a window of 4096 from 82 to 74, and 64 that share none from 182 to 184 and,
+// with 13 registers spilled, from 184 to 210 (32/8 heads, d 128).
 // (launched with 256 threads; the bound: see decode_kernel)
 template <int D, class Block, int STAGES>
 __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs args) {
