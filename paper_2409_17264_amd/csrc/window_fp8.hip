@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <exception>
 #include <vector>
 
 #include "common.h"
@@ -302,6 +303,16 @@ int attn_fp8(const void* q, const medha_kv_cache_fp8* kv, const int32_t* page_ta
                    alloc, context, hip_stream);
 }
 
+// Runs a call whose host memory may not be there: no exception leaves the library.
+template <class F>
+auto guarded(F&& call, decltype(call()) refused) -> decltype(call()) {
+  try {
+    return call();
+  } catch (const std::exception&) {
+    return refused;
+  }
+}
+
 }  // namespace
 }  // namespace medha
 
@@ -327,8 +338,10 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
 size_t medha_window_workspace_bytes(const int32_t* prefix_len, const int32_t* chunk_len,
                                     int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                                     int32_t head_dim, int32_t window, int32_t sinks) {
-  return walk_workspace(prefix_len, chunk_len, batch, num_q_heads, num_kv_heads, head_dim, window,
-                        sinks, false);
+  return guarded([&] {
+    return walk_workspace(prefix_len, chunk_len, batch, num_q_heads, num_kv_heads, head_dim, window,
+                          sinks, false);
+  }, (size_t)0);
 }
 
 int medha_window_attn(const void* q, const medha_kv_cache* kv, const int32_t* page_table,
@@ -337,9 +350,11 @@ int medha_window_attn(const void* q, const medha_kv_cache* kv, const int32_t* pa
                       float softmax_scale, int32_t window, int32_t sinks, int32_t out_type,
                       void* out, float* lse, void* workspace, size_t workspace_bytes,
                       void* hip_stream) {
-  return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
-                   softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
-                   nullptr, nullptr, hip_stream);
+  return guarded([&] {
+    return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
+                     softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
+                     nullptr, nullptr, hip_stream);
+  }, MEDHA_ERR_INVALID_ARG);
 }
 
 int medha_window_attn_alloc(const void* q, const medha_kv_cache* kv, const int32_t* page_table,
@@ -349,17 +364,21 @@ int medha_window_attn_alloc(const void* q, const medha_kv_cache* kv, const int32
                             void* out, float* lse, medha_alloc alloc, void* context,
                             void* hip_stream) {
   if (alloc == nullptr) return MEDHA_ERR_INVALID_ARG;
-  return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
-                   softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
-                   hip_stream);
+  return guarded([&] {
+    return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
+                     softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
+                     hip_stream);
+  }, MEDHA_ERR_INVALID_ARG);
 }
 
 size_t medha_chunked_prefill_fp8_workspace_bytes(const int32_t* prefix_len,
                                                  const int32_t* chunk_len, int32_t batch,
                                                  int32_t num_q_heads, int32_t num_kv_heads,
                                                  int32_t head_dim, int32_t window, int32_t sinks) {
-  return walk_workspace(prefix_len, chunk_len, batch, num_q_heads, num_kv_heads, head_dim, window,
-                        sinks, true);
+  return guarded([&] {
+    return walk_workspace(prefix_len, chunk_len, batch, num_q_heads, num_kv_heads, head_dim, window,
+                          sinks, true);
+  }, (size_t)0);
 }
 
 int medha_chunked_prefill_attn_fp8(const void* q, const medha_kv_cache_fp8* kv,
@@ -369,9 +388,11 @@ int medha_chunked_prefill_attn_fp8(const void* q, const medha_kv_cache_fp8* kv,
                                    int32_t window, int32_t sinks, int32_t out_type, void* out,
                                    float* lse, void* workspace, size_t workspace_bytes,
                                    void* hip_stream) {
-  return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
-                  softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
-                  nullptr, nullptr, hip_stream);
+  return guarded([&] {
+    return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
+                    softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
+                    nullptr, nullptr, hip_stream);
+  }, MEDHA_ERR_INVALID_ARG);
 }
 
 int medha_chunked_prefill_attn_fp8_alloc(const void* q, const medha_kv_cache_fp8* kv,
@@ -382,9 +403,11 @@ int medha_chunked_prefill_attn_fp8_alloc(const void* q, const medha_kv_cache_fp8
                                          float* lse, medha_alloc alloc, void* context,
                                          void* hip_stream) {
   if (alloc == nullptr) return MEDHA_ERR_INVALID_ARG;
-  return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
-                  softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
-                  hip_stream);
+  return guarded([&] {
+    return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
+                    softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
+                    hip_stream);
+  }, MEDHA_ERR_INVALID_ARG);
 }
 
 }  // extern "C"
