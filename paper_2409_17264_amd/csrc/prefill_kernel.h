@@ -123,7 +123,10 @@ typedef const int32_t __attribute__((address_space(4))) * ConstI32Ptr;
 // Which keys a row sees: those up to its limit.
 struct CausalMask {
   int limit;  // last visible key index of the lane's row
-  __device__ __forceinline__ bool sees(int t) const { return t <= limit; }
+  // the score `s` of key t, the lane's f-th of a tile, or -inf if the row does not see it
+  __device__ __forceinline__ float shown(float s, int t, int) const {
+    return t <= limit ? s : -INFINITY;
+  }
 };
 
 // The keys of a walk over all of a sequence's: tile i of the walk is its tile i.
@@ -132,7 +135,7 @@ struct AllKeys {
   __device__ __forceinline__ int tile(int i) const { return i; }
   __device__ __forceinline__ int key0(int t) const { return t * 64; }
   // what a row sees of tile t
-  __device__ __forceinline__ void show(CausalMask&, int) const {}
+  __device__ __forceinline__ void show(CausalMask&, int, int) const {}
   // whether every key of 64-key tile t is read
   __device__ __forceinline__ bool whole(int t) const { return (t + 1) * 64 <= kv_total; }
   // page of the keys from `row` on (16 or fewer, of one page); slot of one of them
@@ -360,7 +363,7 @@ struct RowBlock {
       for (int e = 0; e < 16; ++e) {
         if (MASK) {
           const int t = key0 + kb * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-          s[kb][e] = mask.sees(t) ? s[kb][e] : -INFINITY;
+          s[kb][e] = mask.shown(s[kb][e], t, kb * 16 + e);
         }
         mx = fmaxf(mx, s[kb][e]);
       }
@@ -549,7 +552,7 @@ struct RowBlock {
         for (int f = i * per; f < (i + 1) * per; ++f) {
           if (MASK) {
             const int t = key0 + (f >> 4) * 32 + 8 * ((f & 15) >> 2) + 4 * half + (f & 3);
-            sc[f >> 4][f & 15] = mask.sees(t) ? sc[f >> 4][f & 15] : -INFINITY;
+            sc[f >> 4][f & 15] = mask.shown(sc[f >> 4][f & 15], t, f);
           }
           mx = fmaxf(mx, sc[f >> 4][f & 15]);
         }
@@ -785,7 +788,7 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
         };
         const typename Rows::KSide k_next(rb, ring.base + ((s + 1) % R::kK) * kTile);
         const char* v_cur = ring.base + (s % R::kV) * kTile;  // + the bias in rb.v_off
-        if constexpr (kMask) keys.show(rb.mask, keys.tile(cur));
+        if constexpr (kMask) keys.show(rb.mask, keys.tile(cur), half);
         if constexpr (s & 1)
           rb.template fused<kMask, true, kSpeculate>(k_next, v_cur, s1, s0, keys.key0(keys.tile(cur)), half,
                                                      issue_loads);
@@ -824,7 +827,7 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
   auto final_tile = [&](auto mask) {
     constexpr bool kMask = decltype(mask)::value;
     const char* v_last = ring.base + ((last - kt_a) % R::kV) * kTile;  // + the bias in rb.v_off
-    if constexpr (kMask) keys.show(rb.mask, keys.tile(last));
+    if constexpr (kMask) keys.show(rb.mask, keys.tile(last), half);
     if ((last - kt_a) & 1)
       rb.template fused<kMask, false, false>(typename Rows::KSide(rb, nullptr), v_last, s1, s0, keys.key0(keys.tile(last)), half,
                                                    [](auto) {});
