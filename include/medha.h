@@ -12,6 +12,9 @@
  *   medha_lse_merge             exact combination of partials over disjoint
  *                               key sets.
  *
+ * Beside them: the append into the cache, the same attention behind a sliding
+ * window, and an 8-bit cache with its append, read-back and attention.
+ *
  * Common conventions
  *   - "dev" pointers are device (HBM) memory, "host" pointers ordinary host
  *     memory.  The caller owns every buffer.  The library allocates no device
@@ -310,7 +313,7 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
  *                    medha_chunked_prefill_fp8_workspace_bytes reports for these arguments
  *
  * Arithmetic: the cache's values times q, exact products, accumulated by the matrix cores' 8-bit
- * instructions (a score is off by some 1e-5 of the root mean square of its kind), fp32 softmax
+ * instructions (a score is off by some 5e-6 of the scores' root mean square), fp32 softmax
  * statistics, and P * V as in the bf16 calls.
  * Only tokens that some row of the call sees are read, and only their pages' table entries are
  * used: pages between the first tokens and the windows may be gone, and their entries hold

@@ -1,5 +1,6 @@
 """MI355X-native paged attention for chunked prefill, split-KV decode and the
-log-sum-exp merge of KV-cache parallelism (hand-written HIP behind a C ABI).
+log-sum-exp merge of KV-cache parallelism, an 8-bit KV cache and attention behind
+sliding windows (hand-written HIP behind a C ABI).
 
 The Python layer only marshals arguments; every step runs in the HIP library.
 The library is loaded on first use and a missing library is an error.
