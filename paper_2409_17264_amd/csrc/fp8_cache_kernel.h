@@ -116,8 +116,7 @@ __device__ __forceinline__ uint4 dequantise8(uint2 x, uint32_t byte) {
 
 // One lane per 16 elements of one (token, KV head), for K and for V, so that what it writes to the pools
 // is 16 bytes (13291 tokens at 8 heads, d 128: 18.7 us with 8 elements a lane, 16.4 with 16: 5.0 TB/s).
-// A page id outside
-// [0, num_pages) is skipped: nothing outside the pools is ever written.
+// A page id outside [0, num_pages) is skipped: nothing outside the pools is ever written.
 static __global__ void __launch_bounds__(kThreads) kv_append_fp8_kernel(const Fp8CacheArgs args) {
   const int64_t total = (int64_t)args.total_rows * args.h_kv * args.words_per_row;
   const int64_t step = (int64_t)gridDim.x * kThreads;

@@ -1,13 +1,15 @@
-// Key-split attention over a window of a paged cache, in bf16 or in 8 bits.
+// Attention over a paged cache in 8 bits, and behind a sliding window over either cache.
 //
-// A workgroup owns 32 query rows (token, head-in-group) of one KV head and a range of their walk
-// (KeyWalk, in blocks of 32 keys); its 4 wavefronts take the range's blocks in turn, each with its
-// own online-softmax state, and the four states are combined through LDS at the end.  Each
-// wavefront streams its blocks HBM -> LDS with asynchronous 16-byte loads into a private ring, so
-// the loop has no workgroup barrier.
+//   O[r] = sum_t p[r,t] V[t] / l[r],  p[r,t] = exp(scale * q[r].K[t] - m[r]),  l[r] = sum_t p[r,t],
+//   LSE[r] = m[r] + ln l[r],  t over the keys that row r sees,
 //
-// Only keys that some row of the workgroup sees are read.  The pages between the first tokens and the
-// windows may be gone.
+// in one pass with a running maximum m and sum l (fp32).  Two ways to share the work out:
+//   key_walk_kernel  32 query rows or fewer (decodes): they are read against few rows, so the bytes of
+//                    the cache bound it; the walk is cut into ranges for the whole device to stream.
+//   row_walk_kernel  chunks: 128 or 256 rows against each tile of 64 keys, so the matrix cores and the
+//                    softmax's instructions beside them bound it, not memory.
+// The keys that the rows of a workgroup see come as a KeyWalk.  Only keys that some row of the
+// workgroup sees are read: the pages between the first tokens and the windows may be gone.
 #pragma once
 
 #include <type_traits>
@@ -423,6 +425,14 @@ struct BlockPages {
   }
 };
 
+// A workgroup owns the 32 rows or fewer (token, head in group) of one KV head and a range of their
+// walk, in blocks of 32 keys.  Its 4 wavefronts take the range's blocks in turn, each with a softmax
+// of its own over a ring of its own, so that no barrier holds the stream up; their four states are
+// joined through LDS, those of ranges by split_merge_kernel.
+// Bound by memory: 64 decodes of 4K median at 32/8 heads, d 128, over the 8-bit cache stream 655 MB in
+// 110 us, behind a window of 4096 over the bf16 cache 956 MB in 162 us (both 5.9 TB/s; a large copy
+// reaches 5.1 on the same card).  The matrix pipes are busy 17 % and 9 % of the time.
+//
 // STAGES blocks of every wavefront are in flight while it waits for the first of them.  The loads are
 // non-temporal (see async_stream16), also where sequences share their keys: looking that up in the page
 // table, and a second copy of the walk for it, take 64 decodes that share 8192 keys over the 8-bit cache
@@ -566,7 +576,7 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
   }
 }
 
-// ---------------------------------------------------------------- row-split, bf16 cache
+// ---------------------------------------------------------------- row-split
 
 // The 64-key visits of a walk, for run_tiles(): a tile's number, or its complement where it is visited
 // for first tokens.
@@ -634,11 +644,9 @@ struct TileRows8 : Rows8<D> {
   using R = Fp8Ring<D, NW, SHORT>;
   int k8_off[2 * Base::kParts];  // this lane's 16-byte pieces of key row `col`, within a K tile
   int ks_off;                    // its scale byte within a stage's
-  int wave_page, k_pos, lane;
 
-  __device__ __forceinline__ void init(float scale, int ln, int wave) {
+  __device__ __forceinline__ void init(float scale, int ln) {
     Base::init(scale, ln, R::kV16);
-    lane = ln;
     const int col = ln & 31, half = ln >> 5;
 #pragma unroll
     for (int i = 0; i < 2 * Base::kParts; ++i)
@@ -925,6 +933,13 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
 // Chunks: a workgroup of NW wavefronts owns NW * 32 query rows of one KV head and walks 64-key tiles,
 // as prefill_kernel does, along the tiles of its rows' windows.
 // SHORT: with the short ring, two workgroups to a compute unit.
+// Bound by the matrix cores and the vector instructions of the softmax beside them: 2048 tokens at
+// 32768 over the 8-bit cache (32/8 heads, d 128) take 981 us, 1.16 PFLOP/s (counting 4 d a visible
+// score; a large bf16 matrix product reaches 1.25), over the bf16 cache 951: Q K^T in 8 bits takes
+// the time that bf16 takes (see Rows8), and P V is bf16 in both.  2048 tokens behind a window of 4096
+// over the bf16 cache take 142 us, the matrix pipes busy for 52 % of them and the vector units for 54 %.
+// Eight prompts of 1K median at d 64 behind a window of 1000 take 142 us, 28 % and 68 %: half the head
+// dim leaves a score's softmax as it is, and walks of 18 tiles stay on run_tiles()'s exact route.
 template <int D, int NW, bool kFp8, bool SHORT = false>
 __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   constexpr int NV = SHORT ? 2 : 4;
@@ -948,7 +963,10 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int col = lane & 31, half = lane >> 5;
 
   Rows rb;
-  rb.init(fabsf(args.scale_log2), lane, kFp8 ? wave : Shape::kVBias);
+  if constexpr (kFp8)
+    rb.init(fabsf(args.scale_log2), lane);
+  else
+    rb.init(fabsf(args.scale_log2), lane, Shape::kVBias);
   const int wg_row0 = it.row_tile * Shape::kRowsPerWg;
   const int r = wg_row0 + wave * 32 + col;
   const bool valid = r < n_rows;
