@@ -501,26 +501,29 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
     issue(i, st_issue);
     st_issue = next(st_issue);
   }
-  for (int i = 0; i < n_blocks; ++i) {
-    if (i + STAGES - 1 < n_blocks) {
-      issue(i + STAGES - 1, st_issue);
-      st_issue = next(st_issue);
-      wait_vmcnt<(STAGES - 1) * Block::kLoads>();  // the younger blocks may still fly
-    } else {
-      wait_vmcnt<0>();
+  int i = 0;
+  // (a loop each: with both forms of the step in one, 12 registers of the two-stage bf16 form spill, and
+  // the wait for a reload is one for all loads in flight)
+  auto blocks_to = [&](int end, auto mask_tag) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    for (; i < end; ++i) {
+      if (i + STAGES - 1 < n_blocks) {
+        issue(i + STAGES - 1, st_issue);
+        st_issue = next(st_issue);
+        wait_vmcnt<(STAGES - 1) * Block::kLoads>();  // the younger blocks may still fly
+      } else {
+        wait_vmcnt<0>();
+      }
+      const int b = b_first + i * kWaves, key0 = walk.tile(b) * 32;
+      if (MASK) rb.mask.visit(walk.first_tokens(b), key0, half);
+      block.template step<MASK>(rb, ring + st * Block::kBytes, key0);
+      st = next(st);
+      // every LDS read of the stage has returned before a load refills it
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    const char* stage = ring + st * Block::kBytes;
-    const int b = b_first + i * kWaves, key0 = walk.tile(b) * 32;
-    if (i < n_full) {
-      block.template step<false>(rb, stage, key0);
-    } else {
-      rb.mask.visit(walk.first_tokens(b), key0, half);
-      block.template step<true>(rb, stage, key0);
-    }
-    st = next(st);
-    // every LDS read of the stage has returned before a load refills it
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  }
+  };
+  blocks_to(n_full, std::false_type{});
+  blocks_to(n_blocks, std::true_type{});
 
   // Combine the 4 wavefronts' (m, l, O) over their disjoint keys through LDS.
   const bool direct = sd.n_split == 1;
