@@ -131,6 +131,7 @@ struct CausalMask {
 
 // The keys of a walk over all of a sequence's: tile i of the walk is its tile i.
 struct AllKeys {
+  static constexpr bool kKept = false;
   int kv_total;
   __device__ __forceinline__ int tile(int i) const { return i; }
   __device__ __forceinline__ int key0(int t) const { return t * 64; }
@@ -724,12 +725,22 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
   const int kt_u = kt_mid >= kt_b ? kt_b : kt_a + (kt_mid - kt_a) / R::kRound * R::kRound;
   // Page ids of the next K tile to issue and of the two tiles before it.
   int page_next = 0, page_1 = 0, page_2 = 0;
+  int found = 0, found_1 = 0, found_2 = 0;  // (kKept: those tiles)
   auto next_page = [&](int tile) {
     if (R::kLag > 0) {
       page_2 = page_1;
       page_1 = page_next;
+      found_2 = found_1;
+      found_1 = found;
     }
-    page_next = tile_page<D, NW>(pt, keys.tile(min(tile, last)), keys, wave);
+    found = keys.tile(min(tile, last));
+    page_next = tile_page<D, NW>(pt, found, keys, wave);
+  };
+  auto tile_of = [&](int tile, int kept) {
+    if constexpr (Keys::kKept)
+      return kept;
+    else
+      return keys.tile(min(tile, last));
   };
   // Issues K tile `tile` into K stage k_stage and V tile `tile` - kLag into V stage v_stage, if that
   // is one (tiles past the walk's end: the last one again, harmlessly).  With the short ring V goes
@@ -738,13 +749,13 @@ __device__ __forceinline__ void run_tiles(Rows& rb, const Args& args, ConstI32Pt
     const uint32_t k_lds = ring.lds_addr + decltype(k_stage)::value * kTile;
     const uint32_t v_lds = ring.lds_addr + (R::kK + decltype(v_stage)::value) * kTile;
     if constexpr (R::kLag == 0) {
-      ld.template issue<true, true, kOnce>(args, page_next, keys.tile(min(tile, last)), keys, kv_head, k_lds,
+      ld.template issue<true, true, kOnce>(args, page_next, tile_of(tile, found), keys, kv_head, k_lds,
                                            v_lds);
     } else {
       if constexpr (decltype(v_stage)::value >= 0)
-        ld.template issue<false, true, kOnce>(args, page_2, keys.tile(min(tile - R::kLag, last)), keys,
+        ld.template issue<false, true, kOnce>(args, page_2, tile_of(tile - R::kLag, found_2), keys,
                                               kv_head, 0, v_lds);
-      ld.template issue<true, false, kOnce>(args, page_next, keys.tile(min(tile, last)), keys, kv_head,
+      ld.template issue<true, false, kOnce>(args, page_next, tile_of(tile, found), keys, kv_head,
                                             k_lds, 0);
     }
   };

@@ -87,7 +87,6 @@ struct KeyRange {
   __device__ __forceinline__ int key(int t) const { return min(max(t, from), to); }
   // the page, in the sequence's table, of the 16 keys from t on (a multiple of 16)
   __device__ __forceinline__ int page_index(int t) const { return key(t) >> 4; }
-  __device__ __forceinline__ bool whole(int t, int n) const { return t >= from && t + n - 1 <= to; }
 };
 
 __device__ __forceinline__ void async_load4(const void* base_uniform, uint32_t lane_off,
@@ -584,13 +583,23 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
 // The 64-key visits of a walk, for run_tiles(): a tile's number, or its complement where it is visited
 // for first tokens.
 struct WalkKeys {
+  static constexpr bool kKept = true;  // a tile found when its page is looked up is kept for its loads
   KeyWalk w;
+  int whole_from;               // tiles whose every key the windows reach,
+  uint32_t n_whole, first_whole;  // and of the first tokens'
+  __device__ __forceinline__ explicit WalkKeys(const KeyWalk& walk) : w(walk) {
+    whole_from = (w.lo + 63) >> 6;
+    n_whole = max(0, (w.end >> 6) - whole_from);
+    first_whole = w.first >> 6;
+  }
   __device__ __forceinline__ int tile(int i) const {
     const int t = w.tile(i);
     return w.first_tokens(i) ? ~t : t;
   }
   __device__ __forceinline__ int key0(int v) const { return (v < 0 ? ~v : v) * 64; }
-  __device__ __forceinline__ bool whole(int v) const { return KeyRange(w, v < 0).whole(key0(v), 64); }
+  __device__ __forceinline__ bool whole(int v) const {
+    return (uint32_t)(v - whole_from) < n_whole || v + first_whole < first_whole;
+  }
   __device__ __forceinline__ int page_index(int v, int row) const {
     return KeyRange(w, v < 0).page_index(key0(v) + (row & ~(kPageSize - 1)));
   }
@@ -826,24 +835,27 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
   ld.init(wave, lane);
   Convert cv;
   cv.init(wave, lane);
-  int page_next = 0, page_1 = 0;  // ids of the next tile's page, and of the one before it
+  // the next tile and its page's id, and those before it
+  int tile_next = 0, page_next = 0, tile_1 = 0, page_1 = 0;
   auto next_page = [&](int i) {
-    if (SHORT) page_1 = page_next;
-    const int t = keys.tile(min(i, last));
-    page_next = pt[__builtin_amdgcn_readfirstlane(keys.page_index(t, ld.row0))];
+    if (SHORT) {
+      page_1 = page_next;
+      tile_1 = tile_next;
+    }
+    tile_next = keys.tile(min(i, last));
+    page_next = pt[__builtin_amdgcn_readfirstlane(keys.page_index(tile_next, ld.row0))];
   };
-  // K tile i, and V tile i - kLag if v_stage is one (with the short ring first: the wait for it leaves K
-  // in flight)
-  auto issue = [&](int i, int k_stage, int v_stage) {
+  // the next K tile, and the V tile kLag before it if v_stage is one (with the short ring first: the
+  // wait for it leaves K in flight)
+  auto issue = [&](int k_stage, int v_stage) {
     if constexpr (SHORT) {
       if (v_stage >= 0)
-        ld.template issue<false, true>(args, page_1, keys.tile(min(i - 1, last)), keys, kv_head, ring, 0,
-                                       v_stage, wave, lane);
-      ld.template issue<true, false>(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring,
-                                     k_stage, 0, wave, lane);
+        ld.template issue<false, true>(args, page_1, tile_1, keys, kv_head, ring, 0, v_stage, wave, lane);
+      ld.template issue<true, false>(args, page_next, tile_next, keys, kv_head, ring, k_stage, 0, wave,
+                                     lane);
     } else {
-      ld.template issue<true, true>(args, page_next, keys.tile(min(i, last)), keys, kv_head, ring, k_stage,
-                                    v_stage, wave, lane);
+      ld.template issue<true, true>(args, page_next, tile_next, keys, kv_head, ring, k_stage, v_stage,
+                                    wave, lane);
     }
   };
   auto k_stage = [&](int s) { return lds + s * R::kTile; };
@@ -852,7 +864,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     next_page(kt_a + i);
-    issue(kt_a + i, i, i - R::kLag);
+    issue(i, i - R::kLag);
   }
   next_page(kt_a + 3);
   f32x16 s0[2], s1[2];
@@ -885,7 +897,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
             cv.template read<!kMask && s + 1 < kRound>(lds, k_next, v_next, keys.tile(cur + 1), keys);
           if constexpr (i == Rows::kLoadSlot) {
             asm volatile("" : "+s"(page_next));  // the page id is first needed here, not before
-            issue(cur + 3, (s + 3) % R::kStages, (s + 3 - R::kLag) % R::kVStages);
+            issue((s + 3) % R::kStages, (s + 3 - R::kLag) % R::kVStages);
           }
           if constexpr (i >= kFirst && (i - kFirst) % kStep == 0 &&
                         (i - kFirst) / kStep < Convert::kWords)
@@ -982,8 +994,8 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
 
   const int last_row = min(n_rows, wg_row0 + Shape::kRowsPerWg) - 1;
-  const WalkKeys keys{make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,
-                                args.window, 64)};
+  const WalkKeys keys(make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,
+                                args.window, 64));
   const int kt_begin = split * sd.tiles_per_split;
   const int kt_end = min(keys.w.n, kt_begin + sd.tiles_per_split);
   const int kt_mid = max(kt_begin, min(kt_end, keys.w.n_full));
