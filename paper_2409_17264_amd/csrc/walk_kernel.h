@@ -435,8 +435,7 @@ struct BlockPages {
 // STAGES blocks of every wavefront are in flight while it waits for the first of them.  The loads are
 // non-temporal (see async_stream16), also where sequences share their keys: looking that up in the page
 // table, and a second copy of the walk for it, take 64 decodes that share 8192 keys over the 8-bit cache
-// from 114 to 115 us, behind a window of 4096 from 82 to 74, and 64 that share none from 182 to 184 and,
-// with 13 registers spilled, from 184 to 210 (32/8 heads, d 128).
+// from 114 to 115 us and behind a window of 4096 from 82 to 74, and 64 that share none from 182 to 184.
 // (launched with 256 threads; the bound: see decode_kernel)
 template <int D, class Block, int STAGES>
 __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs args) {
@@ -502,7 +501,7 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
   }
   int i = 0;
   // (a loop each: with both forms of the step in one, 12 registers of the two-stage bf16 form spill, and
-  // the wait for a reload is one for all loads in flight)
+  // the wait for a reload is one for all loads in flight: 16 decodes of 354 at 32/8 heads 16.6 us, 26.9 so)
   auto blocks_to = [&](int end, auto mask_tag) {
     constexpr bool MASK = decltype(mask_tag)::value;
     for (; i < end; ++i) {

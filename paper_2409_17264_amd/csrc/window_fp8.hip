@@ -92,9 +92,10 @@ int move_tokens(bool append, const void* k_rows, const void* v_rows, const medha
 
 // ------------------------------------------------------------------ attention
 
-// Over the bf16 cache a launch that fills the compute units takes the small ring, so that two
-// workgroups share one (64 decodes behind a window of 4096, 32/8 heads, d 128: 290 -> 163 us; 4 of
-// 200000 behind one of 300000, ranges of 65 tiles, 670 -> 376).
+// Over the bf16 cache a launch of more workgroups than compute units takes the small ring, so that two
+// share one (64 decodes of 4K median behind a window of 4096, 32/8 heads, d 128, 141.8 -> 133.5 us; 128
+// of 2K behind 1000 113.9 -> 103.6; 60 of 8K at 8/1 heads behind 300000 73.0 -> 66.9), one of fewer the
+// large (8 of 2K behind 4096, 32/8 heads, 19.9 -> 17.9; 16 of 8K at 8/1 16.7 -> 15.6).
 template <int D>
 hipError_t launch_keys(const LaunchPlan& lp, const WalkArgs& a, int grid, hipStream_t stream) {
   if (a.scale != nullptr)
