@@ -178,11 +178,27 @@ __device__ __forceinline__ int swz8(int row, int chunk) {
   return D == 128 ? (chunk ^ ((row >> 1) & 7)) : (chunk ^ ((row >> 2) & 3));
 }
 
-// Rows of one wavefront against an 8-bit cache.  S^T = K Q^T takes the keys as they are, with their
+// This half's elements of a query row, 32 of every 64: i / 4 counts the 64s.
+template <int D>
+__device__ __forceinline__ void load_q8(uint4 (&raw)[D / 16], const WalkArgs& args, const __bf16* qp,
+                                        bool valid, int half) {
+  const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) {
+    raw[i] = make_uint4(0, 0, 0, 0);
+    if (valid) raw[i] = *reinterpret_cast<const uint4*>(qp + (i / 4) * 64 + half * 32 + (i % 4) * 8);
+    raw[i].x ^= flip; raw[i].y ^= flip; raw[i].z ^= flip; raw[i].w ^= flip;
+  }
+}
+
+// Rows of one wavefront of a chunk against an 8-bit cache.  S^T = K Q^T takes the keys as they are, with their
 // scale byte as the matrix instruction's block scale.  Q is split into two e4m3 parts, q = hi + lo:
 // 4 significant bits each make the 8 of a bf16 number, so nothing of Q is lost (an element below
 // 2^-13 of its row's largest keeps 2^-21 of that).  Two instructions of 32x32x64 take as long as the
-// four of 32x32x16 that bf16 operands take, and no key has to be converted.
+// four of 32x32x16 that bf16 operands take, and no key has to be converted: 64 conversions a tile and
+// wavefront at d 128, to the softmax's 115 vector instructions, or 32 KiB more LDS than two workgroups
+// to a compute unit leave.  The price is the 8-bit instructions' sum, which keeps some 13 bits below its
+// largest product: a score is off by 5e-6 of the scores' rms.
 template <int D>
 struct Rows8 : RowBlock<D, WindowMask> {
   using Base = RowBlock<D, WindowMask>;
@@ -253,7 +269,8 @@ struct Rows8 : RowBlock<D, WindowMask> {
 
 template <int D>
 struct Fp8Block {
-  using Rows = Rows8<D>;
+  using Rows = RowBlock<D, WindowMask>;
+  static constexpr int kParts = D / 64;
   static constexpr int kHalfBytes = 32 * D;
   static constexpr int kBytes = 2 * kHalfBytes + 256;   // K, V, and 64 lanes' worth of scale bytes
   static constexpr int kChunksPerRow = D / 16;
@@ -261,7 +278,7 @@ struct Fp8Block {
   static constexpr int kPerPage = kPageSize / kRowsPerInstr;
   static constexpr int kLoads = 4 * kPerPage + 1;
   uint32_t k_off[kPerPage], v_off[kPerPage];
-  int k8_off[2 * Rows::kParts];    // this lane's pieces of key row lane % 32
+  int k8_off[2 * kParts];          // this lane's pieces of key row lane % 32
   int vt_off[Rows::kDBlocks];      // its place in the transposing reads of a 16-key slice
   int ks_off, r_in, pos, lane, half;
 
@@ -284,7 +301,7 @@ struct Fp8Block {
     }
     const int col = ln & 31;
 #pragma unroll
-    for (int i = 0; i < 2 * Rows::kParts; ++i)
+    for (int i = 0; i < 2 * kParts; ++i)
       k8_off[i] = col * D + swz8<D>(col, (i >> 1) * 4 + half * 2 + (i & 1)) * 16;
     ks_off = (col >> 4) * kScaleBytesPerPage + (col & 15);
     // keys of a slice in the order of P^T's registers: 4*half + 0..3, then the same + 8
@@ -297,15 +314,10 @@ struct Fp8Block {
 
   __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
                                                 bool valid, int half) {
-    const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
     uint4 raw[D / 16];
+    load_q8<D>(raw, args, qp, valid, half);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {  // part i / 4: this half's 32 elements of 64
-      raw[i] = make_uint4(0, 0, 0, 0);
-      if (valid) raw[i] = *reinterpret_cast<const uint4*>(qp + (i / 4) * 64 + half * 32 + (i % 4) * 8);
-      raw[i].x ^= flip; raw[i].y ^= flip; raw[i].z ^= flip; raw[i].w ^= flip;
-    }
-    rb.set_q(raw);
+    for (int i = 0; i < D / 16; ++i) rb.q[i] = __builtin_bit_cast(bf16x8, raw[i]);
   }
 
   template <bool WHOLE, bool kOnce>
@@ -335,6 +347,9 @@ struct Fp8Block {
     async_load4_at(args.scale + b * kScaleBytesPerPage + (lane & 7) * 4, stage + 2 * kHalfBytes);
   }
 
+  // A lane turns its pieces of a key into bf16, scale and all: exact, and the sums are fp32 (an LSE over
+  // 64 keys is off by 2e-7, by 5e-6 with Rows8).  Beside a stream from memory it costs nothing: 64 decodes
+  // of 4K median at 32/8 heads, d 128, 108.7 us either way.
   // The values stay 8 bits wide until the transposing reads have them in registers.  There they
   // become bf16 without their scales, which differ from key to key: the scale of key t is a factor of
   // P[t] instead, a power of two, so nothing is rounded that would not have been.  (With a scale of
@@ -355,17 +370,19 @@ struct Fp8Block {
     for (int i = 0; i < 4; ++i)
       vs[i] = *reinterpret_cast<const uint32_t*>(scales + (i >> 1) * kScaleBytesPerPage + kPageSize +
                                                  (i & 1) * 8 + half * 4);
-    const int ks = (uint8_t)scales[ks_off];
+    const float ks = __builtin_bit_cast(float, (uint32_t)(uint8_t)scales[ks_off] << 23);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-    for (int part = 0; part < Rows::kParts; ++part) {
-      const i32x4 x = *reinterpret_cast<const i32x4*>(stage + k8_off[2 * part]);
-      const i32x4 y = *reinterpret_cast<const i32x4*>(stage + k8_off[2 * part + 1]);
-      const i32x8 a = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rb.hi[part], s, 0, 0, 0, ks, 0, rb.hi_scale);
-      s = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, rb.lo[part], s, 0, 0, 0, ks, 0, rb.lo_scale);
+    for (int i = 0; i < 2 * kParts; ++i) {
+      const uint4 x = *reinterpret_cast<const uint4*>(stage + k8_off[i]);
+      const uint2 a0 = dequantise4(x.x, ks), a1 = dequantise4(x.y, ks);
+      const uint2 b0 = dequantise4(x.z, ks), b1 = dequantise4(x.w, ks);
+      const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y));
+      const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(b0.x, b0.y, b1.x, b1.y));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, rb.q[2 * i], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, rb.q[2 * i + 1], s, 0, 0, 0);
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -429,7 +446,7 @@ struct BlockPages {
 // of its own over a ring of its own, so that no barrier holds the stream up; their four states are
 // joined through LDS, those of ranges by split_merge_kernel.
 // Bound by memory: 64 decodes of 4K median at 32/8 heads, d 128, over the 8-bit cache stream 655 MB in
-// 110 us, behind a window of 4096 over the bf16 cache 956 MB in 162 us (both 5.9 TB/s; a large copy
+// 109 us, behind a window of 4096 over the bf16 cache 956 MB in 162 us (both 5.9 TB/s; a large copy
 // reaches 5.1 on the same card).  The matrix pipes are busy 17 % and 9 % of the time.
 //
 // STAGES blocks of every wavefront are in flight while it waits for the first of them.  The loads are
@@ -948,7 +965,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
 // as prefill_kernel does, along the tiles of its rows' windows.
 // SHORT: with the short ring, two workgroups to a compute unit.
 // Bound by the matrix cores and the vector instructions of the softmax beside them: 2048 tokens at
-// 32768 over the 8-bit cache (32/8 heads, d 128) take 981 us, 1.16 PFLOP/s (counting 4 d a visible
+// 32768 over the 8-bit cache (32/8 heads, d 128) take 972 us, 1.17 PFLOP/s (counting 4 d a visible
 // score; a large bf16 matrix product reaches 1.25), over the bf16 cache 951: Q K^T in 8 bits takes
 // the time that bf16 takes (see Rows8), and P V is bf16 in both.  2048 tokens behind a window of 4096
 // over the bf16 cache take 142 us, the matrix pipes busy for 52 % of them and the vector units for 54 %.
@@ -989,8 +1006,14 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   const int hq = kv_head * gqa + rr % gqa;
   rb.mask.position = sd.prefix_len + tok;
   rb.mask.window = args.window;
-  using Block = std::conditional_t<kFp8, Fp8Block<D>, Bf16Block<D>>;
-  Block::load_q(rb, args, args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D, valid, half);
+  const __bf16* qp = args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D;
+  if constexpr (kFp8) {
+    uint4 raw[D / 16];
+    load_q8<D>(raw, args, qp, valid, half);
+    rb.set_q(raw);
+  } else {
+    Bf16Block<D>::load_q(rb, args, qp, valid, half);
+  }
 
   const int last_row = min(n_rows, wg_row0 + Shape::kRowsPerWg) - 1;
   const WalkKeys keys(make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,

@@ -148,3 +148,20 @@ def test_peaked_and_flat_rows(fp8, window, k_std):
     that are all zero."""
     c = Case(4, 1, 128, [4000], [100], window, 5, fp8, seed=4, k_std=k_std)
     c.check(*c.run())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [(32, 8, 128), (8, 2, 64)])
+@pytest.mark.parametrize("prefix, chunk, window, sinks", [
+    ([776], [1], 129, 1), ([776], [8], 64, 0), ([299] * 8, [1] * 8, None, 0)])
+def test_decodes_over_the_8_bit_cache_add_up_in_fp32(heads, prefix, chunk, window, sinks):
+    """They turn keys into bf16 first, so a score is as exact as over the bf16 cache.  The partial sums of
+    its d products stay below 16 but for rare ones, where a rounding is off by 2^-20 / sqrt(12) rms: d of
+    them sqrt(d) times that, 2.8e-7 after the scale of d^-1/2.  A few roundings of the LSE (below 8: 1.4e-7
+    rms each), an exponential and a logarithm beside them: below 1e-6 rms."""
+    c = Case(*heads, prefix, chunk, window, sinks, True, seed=chunk[0])
+    out, lse = c.run()
+    c.fp8 = False  # (for the bounds: of fp32 sums)
+    want = c.oracle()
+    c.check(out, lse, want)
+    assert np.sqrt(((lse.double().cpu().numpy() - want[1]) ** 2).mean()) < 1e-6
