@@ -968,8 +968,8 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
 // 32768 over the 8-bit cache (32/8 heads, d 128) take 972 us, 1.17 PFLOP/s (counting 4 d a visible
 // score; a large bf16 matrix product reaches 1.25), over the bf16 cache 951: Q K^T in 8 bits takes
 // the time that bf16 takes (see Rows8), and P V is bf16 in both.  2048 tokens behind a window of 4096
-// over the bf16 cache take 142 us, the matrix pipes busy for 52 % of them and the vector units for 54 %.
-// Eight prompts of 1K median at d 64 behind a window of 1000 take 142 us, 28 % and 68 %: half the head
+// over the bf16 cache take 137 us, the matrix pipes and the vector units busy for 53 % of them each.
+// Eight prompts of 1K median at d 64 behind a window of 1000 take 139 us, 29 % and 67 %: half the head
 // dim leaves a score's softmax as it is, and walks of 18 tiles stay on run_tiles()'s exact route.
 template <int D, int NW, bool kFp8, bool SHORT = false>
 __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
