@@ -312,10 +312,8 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
  *   workspace        as for medha_chunked_prefill_attn, of the size that
  *                    medha_chunked_prefill_fp8_workspace_bytes reports for these arguments
  *
- * Arithmetic: the cache's values times q, exact products, accumulated in fp32 for sequences of at
- * most 32 rows a KV head (chunk_len * num_q_heads / num_kv_heads) and by the matrix cores' 8-bit
- * instructions for longer chunks (a score is off by some 5e-6 of the scores' root mean square), fp32
- * softmax statistics, and P * V as in the bf16 calls.
+ * Arithmetic: that of the bf16 calls on the values that the cache stands for, each of which is a bf16
+ * number: exact products, fp32 sums and softmax statistics, probabilities rounded to bf16.
  * Only tokens that some row of the call sees are read, and only their pages' table entries are
  * used: pages between the first tokens and the windows may be gone, and their entries hold
  * anything.  What a row attends to has to be finite for the row's result to be; a NaN or an

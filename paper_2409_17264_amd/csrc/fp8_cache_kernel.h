@@ -66,6 +66,9 @@ __device__ __forceinline__ Fp8Place fp8_place(const Fp8CacheArgs& args, int64_t 
   return p;
 }
 
+// The scale that a byte stands for.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
 // Exponent byte of a row from one lane's 16 elements; the row's lanes (4 or 8 neighbours) agree.
 // Infinities and NaN do not count: they become NaN, and the row's other elements keep their values.
 __device__ __forceinline__ uint32_t row_scale_byte(uint4 x, uint4 y, int lanes) {
@@ -88,7 +91,7 @@ __device__ __forceinline__ s16x2 quantise_pair(s16x2 into, uint32_t w, float sca
 }
 
 __device__ __forceinline__ uint2 quantise8(uint4 x, uint32_t byte) {
-  const float scale = __builtin_bit_cast(float, byte << 23);
+  const float scale = scale_of(byte);
   s16x2 lo = {0, 0}, hi = {0, 0};
   lo = quantise_pair<false>(lo, x.x, scale);
   lo = quantise_pair<true>(lo, x.y, scale);
@@ -108,8 +111,7 @@ __device__ __forceinline__ uint2 dequantise4(uint32_t x, float scale) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false)),
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true)));
 }
-__device__ __forceinline__ uint4 dequantise8(uint2 x, uint32_t byte) {
-  const float scale = __builtin_bit_cast(float, byte << 23);
+__device__ __forceinline__ uint4 dequantise8(uint2 x, float scale) {
   const uint2 a = dequantise4(x.x, scale), b = dequantise4(x.y, scale);
   return make_uint4(a.x, a.y, b.x, b.y);
 }
@@ -153,9 +155,10 @@ __global__ void __launch_bounds__(kThreads) kv_read_fp8_kernel(const Fp8CacheArg
     if (idx >= total) continue;
     uint4 k = make_uint4(0, 0, 0, 0), v = k;
     if (p.valid) {
-      k = dequantise8(static_cast<const uint2*>(args.k_pool)[p.pool_word], args.scale[p.scale_byte]);
+      k = dequantise8(static_cast<const uint2*>(args.k_pool)[p.pool_word],
+                      scale_of(args.scale[p.scale_byte]));
       v = dequantise8(static_cast<const uint2*>(args.v_pool)[p.pool_word],
-                      args.scale[p.scale_byte + kPageSize]);
+                      scale_of(args.scale[p.scale_byte + kPageSize]));
     }
     if (kOnce) {
       __builtin_nontemporal_store(__builtin_bit_cast(u32x4, k),

@@ -178,95 +178,6 @@ __device__ __forceinline__ int swz8(int row, int chunk) {
   return D == 128 ? (chunk ^ ((row >> 1) & 7)) : (chunk ^ ((row >> 2) & 3));
 }
 
-// This half's elements of a query row, 32 of every 64: i / 4 counts the 64s.
-template <int D>
-__device__ __forceinline__ void load_q8(uint4 (&raw)[D / 16], const WalkArgs& args, const __bf16* qp,
-                                        bool valid, int half) {
-  const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    raw[i] = make_uint4(0, 0, 0, 0);
-    if (valid) raw[i] = *reinterpret_cast<const uint4*>(qp + (i / 4) * 64 + half * 32 + (i % 4) * 8);
-    raw[i].x ^= flip; raw[i].y ^= flip; raw[i].z ^= flip; raw[i].w ^= flip;
-  }
-}
-
-// Rows of one wavefront of a chunk against an 8-bit cache.  S^T = K Q^T takes the keys as they are, with their
-// scale byte as the matrix instruction's block scale.  Q is split into two e4m3 parts, q = hi + lo:
-// 4 significant bits each make the 8 of a bf16 number, so nothing of Q is lost (an element below
-// 2^-13 of its row's largest keeps 2^-21 of that).  Two instructions of 32x32x64 take as long as the
-// four of 32x32x16 that bf16 operands take, and no key has to be converted: 64 conversions a tile and
-// wavefront at d 128, to the softmax's 115 vector instructions, or 32 KiB more LDS than two workgroups
-// to a compute unit leave.  The price is the 8-bit instructions' sum, which keeps some 13 bits below its
-// largest product: a score is off by 5e-6 of the scores' rms.
-template <int D>
-struct Rows8 : RowBlock<D, WindowMask> {
-  using Base = RowBlock<D, WindowMask>;
-  static constexpr int kParts = D / 64;
-  i32x8 hi[kParts], lo[kParts];
-  int hi_scale, lo_scale;
-
-  __device__ __forceinline__ void set_q(const uint4 (&raw)[D / 16]) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) top = max(top, 128u * max_exponent(raw[i]));
-    const float both = max_halves(__builtin_bit_cast(float, top << 16));
-    hi_scale = max((int)(__builtin_bit_cast(uint32_t, both) >> 23) - 7, kLeastScaleByte);
-    lo_scale = hi_scale - 4;
-    const float s = __builtin_bit_cast(float, (uint32_t)hi_scale << 23);
-    const float inv = __builtin_bit_cast(float, (uint32_t)(254 - hi_scale) << 23);
-#pragma unroll
-    for (int part = 0; part < kParts; ++part)
-#pragma unroll
-      for (int w = 0; w < 8; ++w) {  // 4 elements each
-        const uint4 x = raw[part * 4 + w / 2];
-        const uint32_t a = w % 2 ? x.z : x.x, b = w % 2 ? x.w : x.y;
-        s16x2 h = {0, 0};
-        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, a), s, false);
-        h = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(h, __builtin_bit_cast(bf16x2, b), s, true);
-        hi[part][w] = __builtin_bit_cast(int, h);
-        const f32x2 h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi[part][w], false);
-        const f32x2 h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi[part][w], true);
-        int r = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (low(a) * inv - h0[0]),
-                                                16.f * (high(a) * inv - h0[1]), 0, false);
-        lo[part][w] = __builtin_amdgcn_cvt_pk_fp8_f32(16.f * (low(b) * inv - h1[0]),
-                                                      16.f * (high(b) * inv - h1[1]), r, true);
-      }
-  }
-
-  // k_lds: rows of D bytes, swizzled; scales: a page's 32 bytes at every kStride.
-  template <int NKB, int kStride = kScaleBytesPerPage>
-  __device__ __forceinline__ void qk(const char* k_lds, const char* scales, int lane,
-                                     f32x16 (&s)[NKB]) const {
-    const int col = lane & 31, half = lane >> 5;
-#pragma unroll
-    for (int kb = 0; kb < NKB; ++kb) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
-      const int row = kb * 32 + col;
-      const int ks = (uint8_t)scales[(row >> 4) * kStride + (row & 15)];
-#pragma unroll
-      for (int part = 0; part < kParts; ++part) {
-        const int c = part * 4 + half * 2;
-        const i32x4 a0 = *reinterpret_cast<const i32x4*>(k_lds + row * D + swz8<D>(row, c) * 16);
-        const i32x4 a1 = *reinterpret_cast<const i32x4*>(k_lds + row * D + swz8<D>(row, c + 1) * 16);
-        const i32x8 a = __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7);
-        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, hi[part], s[kb], 0, 0, 0, ks, 0, hi_scale);
-        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, lo[part], s[kb], 0, 0, 0, ks, 0, lo_scale);
-      }
-    }
-  }
-
- private:
-  static __device__ __forceinline__ float low(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
-  static __device__ __forceinline__ float high(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
-  static __device__ __forceinline__ uint32_t max_exponent(uint4 x) {
-    uint32_t top = 0;
-    for (uint32_t w : {x.x, x.y, x.z, x.w}) top = max(top, max((w >> 7) & 0xffu, (w >> 23) & 0xffu));
-    return top;
-  }
-};
-
 template <int D>
 struct Fp8Block {
   using Rows = RowBlock<D, WindowMask>;
@@ -312,12 +223,17 @@ struct Fp8Block {
       vt_off[db] = row * D + vswz(row, 2 * db + dhalf) * 16 + (l16 & 1) * 8;
   }
 
+  // This half's elements of a query row are 32 of every 64, in the order of the keys' pieces.
   __device__ static __forceinline__ void load_q(Rows& rb, const WalkArgs& args, const __bf16* qp,
                                                 bool valid, int half) {
-    uint4 raw[D / 16];
-    load_q8<D>(raw, args, qp, valid, half);
+    const unsigned flip = args.scale_log2 < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) rb.q[i] = __builtin_bit_cast(bf16x8, raw[i]);
+    for (int i = 0; i < D / 16; ++i) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (valid) raw = *reinterpret_cast<const uint4*>(qp + (i / 4) * 64 + half * 32 + (i % 4) * 8);
+      raw.x ^= flip; raw.y ^= flip; raw.z ^= flip; raw.w ^= flip;
+      rb.q[i] = __builtin_bit_cast(bf16x8, raw);
+    }
   }
 
   template <bool WHOLE, bool kOnce>
@@ -348,8 +264,7 @@ struct Fp8Block {
   }
 
   // A lane turns its pieces of a key into bf16, scale and all: exact, and the sums are fp32 (an LSE over
-  // 64 keys is off by 2e-7, by 5e-6 with Rows8).  Beside a stream from memory it costs nothing: 64 decodes
-  // of 4K median at 32/8 heads, d 128, 108.7 us either way.
+  // 64 keys is off by 2e-7).
   // The values stay 8 bits wide until the transposing reads have them in registers.  There they
   // become bf16 without their scales, which differ from key to key: the scale of key t is a factor of
   // P[t] instead, a power of two, so nothing is rounded that would not have been.  (With a scale of
@@ -370,17 +285,15 @@ struct Fp8Block {
     for (int i = 0; i < 4; ++i)
       vs[i] = *reinterpret_cast<const uint32_t*>(scales + (i >> 1) * kScaleBytesPerPage + kPageSize +
                                                  (i & 1) * 8 + half * 4);
-    const float ks = __builtin_bit_cast(float, (uint32_t)(uint8_t)scales[ks_off] << 23);
+    const float ks = scale_of((uint8_t)scales[ks_off]);
     f32x16 s;
 #pragma unroll
     for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
     for (int i = 0; i < 2 * kParts; ++i) {
       const uint4 x = *reinterpret_cast<const uint4*>(stage + k8_off[i]);
-      const uint2 a0 = dequantise4(x.x, ks), a1 = dequantise4(x.y, ks);
-      const uint2 b0 = dequantise4(x.z, ks), b1 = dequantise4(x.w, ks);
-      const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(a0.x, a0.y, a1.x, a1.y));
-      const bf16x8 b = __builtin_bit_cast(bf16x8, make_uint4(b0.x, b0.y, b1.x, b1.y));
+      const bf16x8 a = __builtin_bit_cast(bf16x8, dequantise8(make_uint2(x.x, x.y), ks));
+      const bf16x8 b = __builtin_bit_cast(bf16x8, dequantise8(make_uint2(x.z, x.w), ks));
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, rb.q[2 * i], s, 0, 0, 0);
       s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, rb.q[2 * i + 1], s, 0, 0, 0);
     }
@@ -399,8 +312,7 @@ struct Fp8Block {
       for (int e = 0; e < 8; ++e) {
         const float pr = rb.prob(s[8 * g + e], m_use);
         ls += pr;
-        const uint32_t byte = (vs[2 * g + (e >> 2)] >> (8 * (e & 3))) & 0xffu;
-        pe[e] = pr * __builtin_bit_cast(float, byte << 23);
+        pe[e] = pr * scale_of((vs[2 * g + (e >> 2)] >> (8 * (e & 3))) & 0xffu);
         // (a key that is not seen weighs nothing, whatever stands in the scale's place)
         if (MASK) pe[e] = pr > 0.f ? pe[e] : 0.f;
       }
@@ -665,58 +577,65 @@ struct Fp8Ring {
   static constexpr int kRowsPerWave = 64 / NW, kLaneBytes = kRowsPerWave * D / 64;
 };
 
-// Rows of one wavefront with what the tile walk needs of them.
+// Rows of one wavefront of a chunk with what the tile walk needs of them.  A lane turns its pieces of a
+// key into bf16, scale and all, as it reads them: exact, and the scores are sums in fp32.  (The matrix
+// instructions that take 8 bits as they are keep some 13 bits below their largest product: with two
+// channels whose products of 512 cancel, scores and LSE were off by 4e-3.  They save 64 conversions a
+// tile: 2048 tokens at 32768, 32/8 heads, d 128, 948 us instead of 1000.)
 template <int D, int NW, bool SHORT>
-struct TileRows8 : Rows8<D> {
-  using Base = Rows8<D>;
+struct TileRows8 : RowBlock<D, WindowMask> {
+  using Base = RowBlock<D, WindowMask>;
   using R = Fp8Ring<D, NW, SHORT>;
-  int k8_off[2 * Base::kParts];  // this lane's 16-byte pieces of key row `col`, within a K tile
-  int ks_off;                    // its scale byte within a stage's
+  static constexpr int kPieces = D / 32;
+  int k8_off[kPieces];  // this lane's 16-byte pieces of key row `col`, within a K tile
+  int ks_off;           // its scale byte within a stage's
 
   __device__ __forceinline__ void init(float scale, int ln) {
     Base::init(scale, ln, R::kV16);
     const int col = ln & 31, half = ln >> 5;
 #pragma unroll
-    for (int i = 0; i < 2 * Base::kParts; ++i)
+    for (int i = 0; i < kPieces; ++i)
       k8_off[i] = col * D + swz8<D>(col, (i >> 1) * 4 + half * 2 + (i & 1)) * 16;
     ks_off = (col >> 4) * R::kScaleStride + (col & 15);
   }
 
-  // Products n = 0, 1, ...: key block n & 1, head-dim part n >> 1, first with the high parts of Q and
-  // then with the low ones.  Each takes the time of two bf16 products: 2 slots of 4.
+  // Slot i: key block i & 1, slice i >> 1, of which two make a piece.
   struct KSide {
     const TileRows8& rb;
     const char* k_lds;
     const char* scales;
-    int ks[2];
-    i32x8 a[2];
+    float ks[2];
+    uint4 raw[2][2];
     __device__ __forceinline__ KSide(const TileRows8& rows, const char* k, const char* s)
         : rb(rows), k_lds(k), scales(s) {}
-    __device__ __forceinline__ void load(int n) {
-      const char* at = k_lds + (n & 1) * 32 * D;
-      const i32x4 x = *reinterpret_cast<const i32x4*>(at + rb.k8_off[2 * (n >> 1)]);
-      const i32x4 y = *reinterpret_cast<const i32x4*>(at + rb.k8_off[2 * (n >> 1) + 1]);
-      a[n & 1] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
     __device__ __forceinline__ void read(int i) {
-      if (i == 0) {
-        ks[0] = (uint8_t)scales[rb.ks_off];
-        ks[1] = (uint8_t)scales[rb.ks_off + 2 * R::kScaleStride];
-        load(0);
-      } else if (i % 4 == 3 && i / 4 + 1 < 2 * Base::kParts) {
-        load(i / 4 + 1);
-      }
+      const int kb = i & 1, piece = i >> 2;
+      if (i < 2) ks[kb] = scale_of((uint8_t)scales[rb.ks_off + kb * 2 * R::kScaleStride]);
+      if (!(i & 2)) raw[kb][piece & 1] = *reinterpret_cast<const uint4*>(k_lds + kb * 32 * D + rb.k8_off[piece]);
+    }
+    __device__ __forceinline__ bf16x8 operand(int i) const {
+      const uint4& x = raw[i & 1][(i >> 2) & 1];
+      return __builtin_bit_cast(bf16x8, dequantise8(i & 2 ? make_uint2(x.z, x.w) : make_uint2(x.x, x.y), ks[i & 1]));
     }
     template <int i>
     __device__ __forceinline__ void multiply(f32x16 (&s)[2]) {
-      if constexpr (i % 2 == 0) {
-        constexpr int n = i / 4, kb = n & 1, part = n >> 1;
-        const i32x8& q = i % 4 == 0 ? rb.hi[part] : rb.lo[part];
-        s[kb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-            a[kb], q, s[kb], 0, 0, 0, ks[kb], 0, i % 4 == 0 ? rb.hi_scale : rb.lo_scale);
-      }
+      s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(i), rb.q[i >> 1], s[i & 1], 0, 0, 0);
     }
   };
+
+  // The scores of a tile alone.
+  __device__ __forceinline__ void qk(const char* k_lds, const char* scales, f32x16 (&s)[2]) const {
+    KSide k(*this, k_lds, scales);
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    auto slot = [&](auto i) {
+      k.read(decltype(i)::value);
+      k.template multiply<decltype(i)::value>(s);
+    };
+    static_for<2 * Base::kSlices>(slot);
+  }
 };
 
 // This wavefront's share of a tile's loads.
@@ -803,7 +722,7 @@ struct Fp8Convert {
     for (int p = 0; p < kPieces; ++p) {
       const int r = row + p * kPieceRows;
       const char* s = lds + R::kS + s_stage * R::kScales + (r >> 4) * R::kScaleStride + kPageSize;
-      scale[p] = __builtin_bit_cast(float, (uint32_t)(uint8_t)s[WHOLE ? r & 15 : keys.slot(tile, r)] << 23);
+      scale[p] = scale_of((uint8_t)s[WHOLE ? r & 15 : keys.slot(tile, r)]);
       if constexpr (kPieceWords == 4) {
         const uint4 x = *reinterpret_cast<const uint4*>(in + p * kPieceRows * D);
         raw[4 * p] = x.x; raw[4 * p + 1] = x.y; raw[4 * p + 2] = x.z; raw[4 * p + 3] = x.w;
@@ -890,7 +809,7 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
   auto convert_all = [&](auto w) { cv.template convert<decltype(w)::value>(lds, 0); };
   cv.template read<false>(lds, 0, 0, keys.tile(kt_a), keys);
   static_for<Convert::kWords>(convert_all);
-  rb.template qk<2, R::kScaleStride>(k_stage(0), scales(0), lane, s0);
+  rb.qk(k_stage(0), scales(0), s0);
   if (kt_u > kt_a) {
     float mx = -INFINITY;
 #pragma unroll
@@ -965,9 +884,8 @@ __device__ __forceinline__ void run_tiles8(TileRows8<D, NW, SHORT>& rb, const Wa
 // as prefill_kernel does, along the tiles of its rows' windows.
 // SHORT: with the short ring, two workgroups to a compute unit.
 // Bound by the matrix cores and the vector instructions of the softmax beside them: 2048 tokens at
-// 32768 over the 8-bit cache (32/8 heads, d 128) take 972 us, 1.17 PFLOP/s (counting 4 d a visible
-// score; a large bf16 matrix product reaches 1.25), over the bf16 cache 951: Q K^T in 8 bits takes
-// the time that bf16 takes (see Rows8), and P V is bf16 in both.  2048 tokens behind a window of 4096
+// 32768 over the 8-bit cache (32/8 heads, d 128) take 1000 us, 1.13 PFLOP/s (counting 4 d a visible
+// score; a large bf16 matrix product reaches 1.25), over the bf16 cache 951.  2048 tokens behind a window of 4096
 // over the bf16 cache take 137 us, the matrix pipes and the vector units busy for 53 % of them each.
 // Eight prompts of 1K median at d 64 behind a window of 1000 take 139 us, 29 % and 67 %: half the head
 // dim leaves a score's softmax as it is, and walks of 18 tiles stay on run_tiles()'s exact route.
@@ -1007,13 +925,7 @@ __global__ void __launch_bounds__(512) row_walk_kernel(const WalkArgs args) {
   rb.mask.position = sd.prefix_len + tok;
   rb.mask.window = args.window;
   const __bf16* qp = args.q + ((int64_t)(sd.q_row + tok) * args.h_q + hq) * D;
-  if constexpr (kFp8) {
-    uint4 raw[D / 16];
-    load_q8<D>(raw, args, qp, valid, half);
-    rb.set_q(raw);
-  } else {
-    Bf16Block<D>::load_q(rb, args, qp, valid, half);
-  }
+  std::conditional_t<kFp8, Fp8Block<D>, Bf16Block<D>>::load_q(rb, args, qp, valid, half);
 
   const int last_row = min(n_rows, wg_row0 + Shape::kRowsPerWg) - 1;
   const WalkKeys keys(make_walk(sd.prefix_len + wg_row0 / gqa, sd.prefix_len + last_row / gqa,
