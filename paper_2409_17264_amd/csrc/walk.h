@@ -54,4 +54,19 @@ __host__ __device__ inline KeyWalk make_walk(int32_t p_a, int32_t p_b, const Win
   return k;
 }
 
+// Whether every key of a visit's 64-key tile is read: `v` is a tile's number, or its complement where it
+// is visited for first tokens.
+struct WholeTiles {
+  int32_t from;         // tiles whose every key the windows reach,
+  uint32_t n, n_first;  // and of the first tokens'
+  __host__ __device__ __forceinline__ explicit WholeTiles(const KeyWalk& w) {
+    from = (int32_t)(((uint32_t)w.lo + 63) >> 6);  // (lo + 63 may pass 2^31 - 1)
+    n = w.end >> 6 > from ? (w.end >> 6) - from : 0;
+    n_first = w.first >> 6;
+  }
+  __host__ __device__ __forceinline__ bool holds(int32_t v) const {
+    return (uint32_t)(v - from) < n || (uint32_t)v + n_first < n_first;
+  }
+};
+
 }  // namespace medha

@@ -513,21 +513,14 @@ __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs a
 struct WalkKeys {
   static constexpr bool kKept = true;  // a tile found when its page is looked up is kept for its loads
   KeyWalk w;
-  int whole_from;               // tiles whose every key the windows reach,
-  uint32_t n_whole, first_whole;  // and of the first tokens'
-  __device__ __forceinline__ explicit WalkKeys(const KeyWalk& walk) : w(walk) {
-    whole_from = (w.lo + 63) >> 6;
-    n_whole = max(0, (w.end >> 6) - whole_from);
-    first_whole = w.first >> 6;
-  }
+  WholeTiles whole_tiles;
+  __device__ __forceinline__ explicit WalkKeys(const KeyWalk& walk) : w(walk), whole_tiles(walk) {}
   __device__ __forceinline__ int tile(int i) const {
     const int t = w.tile(i);
     return w.first_tokens(i) ? ~t : t;
   }
   __device__ __forceinline__ int key0(int v) const { return (v < 0 ? ~v : v) * 64; }
-  __device__ __forceinline__ bool whole(int v) const {
-    return (uint32_t)(v - whole_from) < n_whole || v + first_whole < first_whole;
-  }
+  __device__ __forceinline__ bool whole(int v) const { return whole_tiles.holds(v); }
   __device__ __forceinline__ int page_index(int v, int row) const {
     return KeyRange(w, v < 0).page_index(key0(v) + (row & ~(kPageSize - 1)));
   }
