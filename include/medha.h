@@ -43,8 +43,9 @@
  *     has less scratch and is accepted all the same may cut the keys at other
  *     places, which moves roundings.
  *   - Return value: MEDHA_OK (0) or a negative error code.  On an error
- *     detected by argument validation nothing is enqueued and no output byte
- *     is written.
+ *     detected by argument validation, and on MEDHA_ERR_MEMORY, nothing is
+ *     enqueued and no output byte is written.  Workspace queries return 0 for
+ *     what their call would refuse with these codes.
  */
 #ifndef MEDHA_H_
 #define MEDHA_H_
@@ -61,6 +62,7 @@ extern "C" {
 #define MEDHA_ERR_UNSUPPORTED (-2)  /* page_size != 16, head_dim not 64/128                     */
 #define MEDHA_ERR_WORKSPACE (-3)    /* workspace missing, misaligned or too small              */
 #define MEDHA_ERR_HIP (-4)          /* a HIP runtime call failed                               */
+#define MEDHA_ERR_MEMORY (-5)       /* no host memory for a call's plan (windowed calls, 8-bit cache) */
 
 /* Paged KV cache descriptor (host struct holding device pointers).  The pools are read-only
  * for every call except medha_kv_append. */

@@ -298,6 +298,7 @@ const char* medha_strerror(int code) {
     case MEDHA_ERR_UNSUPPORTED: return "unsupported shape (page size must be 16, head_dim 64 or 128)";
     case MEDHA_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case MEDHA_ERR_HIP: return "HIP runtime error";
+    case MEDHA_ERR_MEMORY: return "no host memory for the call's plan";
     default: return "unknown error code";
   }
 }

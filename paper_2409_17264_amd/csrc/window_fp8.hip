@@ -355,7 +355,7 @@ int medha_window_attn(const void* q, const medha_kv_cache* kv, const int32_t* pa
     return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
                      softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
                      nullptr, nullptr, hip_stream);
-  }, MEDHA_ERR_INVALID_ARG);
+  }, MEDHA_ERR_MEMORY);
 }
 
 int medha_window_attn_alloc(const void* q, const medha_kv_cache* kv, const int32_t* page_table,
@@ -369,7 +369,7 @@ int medha_window_attn_alloc(const void* q, const medha_kv_cache* kv, const int32
     return attn_bf16(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
                      softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
                      hip_stream);
-  }, MEDHA_ERR_INVALID_ARG);
+  }, MEDHA_ERR_MEMORY);
 }
 
 size_t medha_chunked_prefill_fp8_workspace_bytes(const int32_t* prefix_len,
@@ -393,7 +393,7 @@ int medha_chunked_prefill_attn_fp8(const void* q, const medha_kv_cache_fp8* kv,
     return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
                     softmax_scale, window, sinks, out_type, out, lse, workspace, workspace_bytes,
                     nullptr, nullptr, hip_stream);
-  }, MEDHA_ERR_INVALID_ARG);
+  }, MEDHA_ERR_MEMORY);
 }
 
 int medha_chunked_prefill_attn_fp8_alloc(const void* q, const medha_kv_cache_fp8* kv,
@@ -408,7 +408,7 @@ int medha_chunked_prefill_attn_fp8_alloc(const void* q, const medha_kv_cache_fp8
     return attn_fp8(q, kv, page_table, page_table_offs, prefix_len, chunk_len, batch, num_q_heads,
                     softmax_scale, window, sinks, out_type, out, lse, nullptr, 0, alloc, context,
                     hip_stream);
-  }, MEDHA_ERR_INVALID_ARG);
+  }, MEDHA_ERR_MEMORY);
 }
 
 }  // extern "C"
