@@ -259,7 +259,8 @@ int medha_kv_append(const void* k_new, const void* v_new, const medha_kv_cache* 
  * largest finite magnitude,
  *     byte  = max(E - 7, 10)
  *     value = x * 2^(127 - byte), rounded to the nearest e4m3 value, ties to even.
- * The largest value lies in [128, 256]: nothing saturates.  An element is off by at most 2^-4 of
+ * The largest value lies in [128, 256]: nothing saturates.  Bytes run from 10 to 247, and the calls that
+ * read the cache take no others where a row is seen.  An element is off by at most 2^-4 of
  * itself, or by 2^-10 * 2^(byte - 127) where that is more (elements below 2^-13 of the row's
  * largest).  Infinities and NaN become NaN (of either sign); magnitudes above 1.875 * 2^127 become that.
  */

@@ -267,8 +267,9 @@ struct Fp8Block {
   // 64 keys is off by 2e-7).
   // The values stay 8 bits wide until the transposing reads have them in registers.  There they
   // become bf16 without their scales, which differ from key to key: the scale of key t is a factor of
-  // P[t] instead, a power of two, so nothing is rounded that would not have been.  (With a scale of
-  // 2^-117 a probability below 2^-9 is lost to bf16's range: values below 2^-109.)
+  // P[t] instead, a power of two, so nothing is rounded that would not have been: the values, up to 2^8,
+  // give P 7 powers of two from their own range, which puts the scales, 2^-117 to 2^120, at 2^-110 to
+  // 2^127, and a probability keeps bf16's 8 bits down to 2^-16 of its row's largest at the least of them.
   template <bool MASK>
   __device__ __forceinline__ void step(Rows& rb, const char* stage, int key0) const {
     const char* scales = stage + 2 * kHalfBytes;
@@ -312,14 +313,14 @@ struct Fp8Block {
       for (int e = 0; e < 8; ++e) {
         const float pr = rb.prob(s[8 * g + e], m_use);
         ls += pr;
-        pe[e] = pr * scale_of((vs[2 * g + (e >> 2)] >> (8 * (e & 3))) & 0xffu);
+        pe[e] = pr * scale_of(((vs[2 * g + (e >> 2)] >> (8 * (e & 3))) & 0xffu) + 7);
         // (a key that is not seen weighs nothing, whatever stands in the scale's place)
         if (MASK) pe[e] = pr > 0.f ? pe[e] : 0.f;
       }
       const bf16x8 pv = __builtin_convertvector(pe, bf16x8);
 #pragma unroll
       for (int db = 0; db < Rows::kDBlocks; ++db) {
-        const uint2 lo = dequantise4(raw[g][db][0], 1.f), hi = dequantise4(raw[g][db][1], 1.f);
+        const uint2 lo = dequantise4(raw[g][db][0], 0x1p-7f), hi = dequantise4(raw[g][db][1], 0x1p-7f);
         const bf16x8 v = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
         rb.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pv, rb.o[db], 0, 0, 0);
       }
