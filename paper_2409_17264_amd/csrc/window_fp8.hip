@@ -176,9 +176,11 @@ hipError_t launch_walks(const LaunchPlan& lp, WalkArgs& a, hipStream_t stream) {
 
 // The window of a call: 0 keys mean none, where that is allowed.
 bool window_of(int32_t keys, int32_t sinks, bool optional, Window& w) {
-  if (keys < (optional ? 0 : 1) || sinks < 0) return false;
-  w.keys = keys > 0 ? keys : INT32_MAX;
-  w.sinks = keys > 0 ? sinks : 0;
+  w = Window{};
+  if (optional && keys == 0) return true;
+  if (keys < 1 || sinks < 0) return false;
+  w.keys = keys;
+  w.sinks = sinks;
   return true;
 }
 
