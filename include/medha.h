@@ -35,7 +35,8 @@
  *     num_kv_heads).
  *   - Scores are softmax_scale * <q, k>; LSE is the natural logarithm of the sum
  *     of exp(score) over the keys attended to.  A row that attends to no key
- *     gets O = 0 and LSE = -inf.
+ *     gets O = 0 and LSE = -inf.  What a row attends to has to be finite for its
+ *     results to be defined (windowed calls and the 8-bit cache: see there).
  *   - Arithmetic: bf16 operands, fp32 accumulation (matrix cores), fp32 softmax
  *     statistics; probabilities are rounded to bf16 before the P*V product.
  *     For one input and one device the result is bitwise reproducible, with
@@ -306,7 +307,8 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
  * p of a sequence attends to keys t <= p with  t > p - window  or  t < sinks  (window 0: to all
  * t <= p; sinks is not looked at).  The other arguments, the batches and the layouts are those of
  * medha_chunked_prefill_attn.  O and LSE of a shard that lies before the query are those of the
- * sequence (prefix_len = kv_len - 1, chunk_len 1) and merge with medha_lse_merge as others do.
+ * sequence (prefix_len = kv_len - 1, chunk_len 1) and merge with medha_lse_merge as others do; an
+ * empty shard is left out of the merge.
  *
  *   window           keys a row sees up to and with its own, >= 1, or 0
  *   sinks            first tokens of the sequence that every row sees, >= 0
@@ -319,8 +321,9 @@ int medha_kv_read_fp8(const medha_kv_cache_fp8* kv, const int32_t* page_table,
  * number: exact products, fp32 sums and softmax statistics, probabilities rounded to bf16.
  * Only tokens that some row of the call sees are read, and only their pages' table entries are
  * used: pages between the first tokens and the windows may be gone, and their entries hold
- * anything.  What a row attends to has to be finite for the row's result to be; a NaN or an
- * infinity among the keys or values that the call reads may reach any row of its sequence.
+ * anything.  What a row attends to has to be finite for the row's result to be: a NaN in a key that
+ * it sees makes all of its result NaN, one in a value that element of O.  A NaN or an infinity among the
+ * keys or values that the call reads may reach any row of its sequence, and of no other.
  */
 #define MEDHA_OUT_FP32 0
 #define MEDHA_OUT_BF16 1

@@ -97,10 +97,10 @@ inline WalkCost walk_cost(int head_dim, int q_blocks) {
 // measured 1.02) and a twelfth more at 128 (a pair 1.11, measured 1.05): where walks are long, a
 // small form wins by the whole round that it saves or not at all.
 constexpr WalkCost kAloneCost[2] = {{0.65, 9.0, 1}, {1.25, 8.0, 1}}, kPairedCost{1.85, 8.0, 2};
-// In pairs over the 8-bit cache, where both read half as much: a pair of long walks takes 1.04 to 1.07
-// of the large form's time (1500 tokens at 65536, 32/8 heads, 1479 us large, 1543 in pairs; 1000 at
-// 131072 1874 and 1997), and wins where 128 rows fit better (111 at 524291, 16/2 heads, 493 -> 465,
-// 8/1 257 -> 246).
+// In pairs over the 8-bit cache, where both read half as much: a pair of long walks takes 1.03 to 1.05
+// of the large form's time (1500 tokens at 65536, 32/8 heads, 1482 us large, 1536 in pairs; 1000 at
+// 131072 1895 and 1997), and wins where 128 rows fit better (111 at 524291, 16/2 heads, 480 -> 466,
+// 8/1 252 -> 244; 1353 at 19556, 16/2, 257 -> 232).  It misses at 777 of 20000, 32/8: 277 -> 285.
 constexpr WalkCost kPairedCostFp8{1.75, 8.0, 2};
 
 constexpr int64_t kShortPairedTiles = 10;

@@ -359,13 +359,15 @@ struct BlockPages {
 // of its own over a ring of its own, so that no barrier holds the stream up; their four states are
 // joined through LDS, those of ranges by split_merge_kernel.
 // Bound by memory: 64 decodes of 4K median at 32/8 heads, d 128, over the 8-bit cache stream 655 MB in
-// 109 us, behind a window of 4096 over the bf16 cache 956 MB in 162 us (both 5.9 TB/s; a large copy
+// 109 us, behind a window of 4096 over the bf16 cache 956 MB in 162 us (6.0 and 5.9 TB/s; a large copy
 // reaches 5.1 on the same card).  The matrix pipes are busy 17 % and 9 % of the time.
 //
 // STAGES blocks of every wavefront are in flight while it waits for the first of them.  The loads are
 // non-temporal (see async_stream16), also where sequences share their keys: looking that up in the page
 // table, and a second copy of the walk for it, take 64 decodes that share 8192 keys over the 8-bit cache
 // from 114 to 115 us and behind a window of 4096 from 82 to 74, and 64 that share none from 182 to 184.
+// (Behind a window sequences share what they read only until they are a window past their common prefix:
+// of a server's decodes the few.)
 // (launched with 256 threads; the bound: see decode_kernel)
 template <int D, class Block, int STAGES>
 __global__ void __launch_bounds__(2 * kThreads) key_walk_kernel(const WalkArgs args) {
