@@ -24,8 +24,6 @@
 namespace medha {
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 struct WalkArgs {
   const __bf16* q;
